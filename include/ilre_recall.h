@@ -39,7 +39,9 @@ enum ilre_status {
   ILRE_ERR_DEVICE_WAIT = -7,  /* a bounded wait inside a kernel gave up (see _status)        */
   ILRE_ERR_QUOTA = -8,        /* a combination ran out of candidates (cannot happen for valid */
                               /* inputs; reported by _status)                                */
-  ILRE_ERR_NOMEM = -9         /* workspace allocation failed in create()                     */
+  ILRE_ERR_NOMEM = -9,        /* workspace allocation failed in create()                     */
+  ILRE_ERR_BATCH = -10        /* lengths or page numbers on the device out of range (reported */
+                              /* by ilre_paged_status)                                       */
 };
 
 /* Capacities fixed at create(); run() never allocates. */
@@ -361,6 +363,176 @@ int ilre_recall_destroy(ilre_recall_t* h);
 #define ILRE_NOALLOC_MAX_L 1048576
 int ilre_topk_positions_noalloc(const float* scores_dev, int64_t L, int32_t k,
                                 int32_t* out_idx_dev, void* cuda_stream);
+
+/*
+ * Rotary positions (Eq. 3) in the forms that models serve with.  Channel pairs of the first
+ * rotary_dim channels of every head turn by position * f_i, i = 0 .. rotary_dim/2 - 1:
+ *   ILRE_ROPE_HALF         pair (i, i + rotary_dim/2)   (the layout of ilre_recall_fill_keys)
+ *   ILRE_ROPE_INTERLEAVED  pair (2i, 2i + 1)
+ * the channels behind them are copied.  With b_i = theta^(-2i/rotary_dim):
+ *   ILRE_ROPE_PLAIN   f_i = b_i
+ *   ILRE_ROPE_LINEAR  f_i = b_i / factor
+ *   ILRE_ROPE_BANDED  by the wavelength w = 2 pi / b_i: t = (orig_len/w - low) / (high - low) clamped
+ *                     to [0, 1], f_i = (1 - t) b_i / factor + t b_i
+ *   ILRE_ROPE_YARN    d(n) = rotary_dim ln(orig_len / (2 pi n)) / (2 ln theta), lo = max(floor(d(high)), 0),
+ *                     hi = min(ceil(d(low)), rotary_dim - 1), r = (i - lo) / max(hi - lo, 0.001) clamped to
+ *                     [0, 1], f_i = r b_i / factor + (1 - r) b_i
+ * The rotated channels are multiplied by attn_factor (0: 0.1 ln(factor) + 1 with ILRE_ROPE_YARN, else 1).
+ * low < high are the frequency factors of ILRE_ROPE_BANDED and the turns of ILRE_ROPE_YARN (there also
+ * called beta_slow and beta_fast).  Angles are reduced in double precision, so far positions lose nothing.
+ */
+#define ILRE_BF16 0
+#define ILRE_F16 1
+#define ILRE_ROPE_HALF 0
+#define ILRE_ROPE_INTERLEAVED 1
+#define ILRE_ROPE_PLAIN 0
+#define ILRE_ROPE_LINEAR 1
+#define ILRE_ROPE_BANDED 2
+#define ILRE_ROPE_YARN 3
+typedef struct {
+  double theta;              /* > 1                                                           */
+  int32_t rotary_dim;        /* 16 .. min(head_dim, 256), a multiple of 16                    */
+  int32_t layout;            /* ILRE_ROPE_HALF or ILRE_ROPE_INTERLEAVED                       */
+  int32_t scaling;           /* ILRE_ROPE_PLAIN ...                                           */
+  double factor;             /* >= 1 with a scaling                                           */
+  double orig_len;           /* >= 1 with ILRE_ROPE_BANDED and ILRE_ROPE_YARN                 */
+  double low, high;          /* 0 < low < high with those two                                 */
+  double attn_factor;        /* >= 0                                                          */
+} ilre_rope_spec_t;
+
+/*
+ * Rotates x [n_tokens][n_heads][head_dim] (dtype ILRE_BF16 or ILRE_F16; heads contiguous, x_stride
+ * elements from token to token) by the tokens' positions pos_dev (int32 [n_tokens], any value) into out
+ * (out_stride from token to token; out may be x with the same stride, else they do not overlap).
+ * transposed != 0 applies the transposed map, which is the gradient's: the angles are negated and
+ * attn_factor still multiplies.  head_dim a multiple of 16 up to 1024 (ILRE_ERR_UNSUPPORTED), both
+ * pointers 16-byte aligned and both strides multiples of 8 elements (ILRE_ERR_ALIGNMENT), strides at least
+ * n_heads * head_dim.  Arithmetic in fp32, one rounding.  No handle; the current device; asynchronous
+ * on cuda_stream; may be captured.
+ */
+int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride, void* out_dev,
+              int64_t out_stride, const int32_t* pos_dev, int64_t n_tokens, int32_t n_heads,
+              int32_t head_dim, int32_t dtype, int32_t transposed, void* cuda_stream);
+
+/*
+ * Paged key/value cache: what the compressed prompt (Section 3.3, the last step, hands it to "the
+ * inference engine") is answered from.  Rows of a sequence lie in pages of page_size rows; the
+ * block table gives the page of each run.  A page of keys or values is a run of a cache in the layout of
+ * ilre_recall_run, [page_size][n_kv_heads][128], so a cache [L][n_kv_heads][128] is a pool of
+ * L / page_size pages.
+ *
+ * The handle owns the workspace of the split work (about 60 MB) and nothing of the cache.  It may be
+ * used from one host thread and one stream at a time; calls captured into graphs use its workspace
+ * too, so graphs of one handle must not run at the same time as each other or as other calls of it.
+ */
+typedef struct ilre_paged ilre_paged_t;
+
+typedef struct {
+  int32_t n_kv_heads;        /* 1 .. 1024                                                    */
+  int32_t n_q_heads;         /* query head h reads kv head h / (n_q/n_kv); n_q/n_kv <= 128   */
+  int32_t head_dim;          /* must be 128                                                  */
+  int32_t page_size;         /* 16, 32, 64, ... 1024                                         */
+  int32_t dtype;             /* ILRE_BF16 or ILRE_F16: q, k, v, the pools and the output     */
+  int32_t max_seqs;          /* largest number of sequences of a batch, <= 65535             */
+  int32_t device;            /* CUDA device ordinal                                          */
+} ilre_paged_config_t;
+
+/*
+ * A batch of sequences.  The numbers are read on the host, the arrays on the device when the kernels
+ * run (so a captured call may be replayed with other lengths and tables).  Sequence i has the new tokens
+ * q_start[i] .. q_start[i+1] - 1 and kv_len[i] cached rows, those of its new tokens among them and last:
+ * its new token j is row kv_len[i] - n_i + j and sees the rows up to itself.  Row t lies in page
+ * block_table[i][t / page_size] at t % page_size.  Tokens behind q_start[n_seqs] belong to no sequence
+ * and are left as they are; a sequence may have no new tokens, or no rows.
+ * Checked on the device: 0 <= q_start[i] <= q_start[i+1] <= n_tokens, n_i <= max_q_len, 0 <= kv_len[i] <=
+ * max_blocks * page_size, 0 <= page < n_pages for the pages of rows below kv_len[i].  A sequence whose
+ * lengths are out of range is left out; a row whose page is out of range is not written, counts as
+ * zeros where it is read; ilre_paged_status then returns ILRE_ERR_BATCH.
+ */
+typedef struct {
+  int32_t n_seqs;                    /* 0 .. max_seqs                                        */
+  int32_t n_tokens;                  /* rows of q                                            */
+  int32_t max_q_len;                 /* most new tokens of one sequence (bounds the launches) */
+  int32_t max_blocks;                /* row length of the block table; max_blocks * page_size < 2^31 - 2048 */
+  const int32_t* q_start_dev;        /* int32 [n_seqs + 1]                                   */
+  const int32_t* kv_len_dev;         /* int32 [n_seqs]                                       */
+  const int32_t* block_table_dev;    /* int32 [n_seqs][max_blocks]                           */
+} ilre_paged_batch_t;
+
+/* Pools of n_pages pages.  Strides in elements from page to page (0: page_size * n_kv_heads * 128,
+ * pages back to back); multiples of 8, not less than that. */
+typedef struct {
+  void* k_dev;                       /* [n_pages][page_size][n_kv_heads][128]                */
+  void* v_dev;                       /* same                                                 */
+  float* w_dev;                      /* fp32 [n_pages][n_kv_heads][page_size]: accumulated weights */
+  int64_t k_page_stride, v_page_stride;
+  int32_t n_pages;
+} ilre_paged_pool_t;
+
+int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out);
+
+/*
+ * New tokens into the cache: k [n_tokens][n_kv_heads][128] is rotated by the tokens' positions (ilre_rope)
+ * and v copied to the rows of the new tokens, their accumulated weights (w_dev, if given) are set to
+ * 0, and q [n_tokens][n_q_heads][128] is rotated into q_out.  Strides in elements from token to token
+ * (multiples of 8; q_out may be q with its stride).  q_dev and q_out_dev may both be NULL, and spec NULL copies
+ * without a rotation (pos_dev may then be NULL).  Positions are given apart from the rows because after an
+ * eviction they differ.  kv_len[i] >= n_i (else the sequence is left out and reported); rows that are
+ * written belong to one sequence, on one page.
+ */
+int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const ilre_rope_spec_t* spec,
+                      const int32_t* pos_dev, const void* q_dev, int64_t q_stride, void* q_out_dev,
+                      int64_t q_out_stride, const void* k_dev, int64_t k_stride, const void* v_dev,
+                      int64_t v_stride, const ilre_paged_pool_t* pool, void* cuda_stream);
+
+/*
+ * Attention of the new tokens over the cache (Eq. 2's step for every layer behind the compression):
+ *   out[j, h, :] = sum_t softmax_t(q[j, h, :] . k[t, kv(h), :] / sqrt(128)) v[t, kv(h), :],  t visible to j
+ *   lse_out[j, h] = ln sum_t exp(q . k / sqrt(128))      (fp32 [n_tokens][n_q_heads], NULL to skip)
+ * q_dev [n_tokens][n_q_heads][128] with q_stride elements from token to token, out_dev contiguous.  A token
+ * that sees nothing (kv_len[i] < n_i) gets zeros and lse -infinity.  Rows at kv_len[i] and beyond may hold
+ * anything, NaN included; values of rows below it must be finite.  Pages may be shared.  Products on
+ * the tensor cores, fp32 sums; the probabilities are rounded to the cache's type before they multiply
+ * the values, as the output is.
+ */
+int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev,
+                         int64_t q_stride, const ilre_paged_pool_t* pool, void* out_dev,
+                         float* lse_out_dev, void* cuda_stream);
+
+/*
+ * Attention weight that every cached row received from the batch's new tokens, added to the pool:
+ *   w[t, g] += sum over the heads h of kv head g and the new tokens j that see t of
+ *              exp(q[j, h, :] . k[t, g, :] / sqrt(128) - lse[j, h])
+ * with q and lse as in ilre_paged_attention.  Sums in fp32; a page that several sequences of the batch
+ * share receives all of theirs (in an order that may vary; without sharing results repeat bit by bit).
+ */
+int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev,
+                          int64_t q_stride, const float* lse_dev, const ilre_paged_pool_t* pool,
+                          void* cuda_stream);
+
+/*
+ * Eviction: cuts every sequence of more than `budget` rows to `budget`.  Kept are its first n_sink rows,
+ * its last n_recent rows and, of those between, the budget - n_sink - n_recent rows of largest accumulated weight
+ * (equal weights: the lower row).  per_head != 0: each kv head by its own weights; else one choice for all, by
+ * the weights' sum over the kv heads (formed in fp64, rounded to fp32).  The kept rows' keys, values and
+ * weights become rows 0, 1, ... in their old order: in the sequence's own pages (dst_table_dev NULL; their
+ * pages must then be on one place of one sequence's table only), or in the pages of dst_table_dev
+ * [n_seqs][dst_blocks] (dst_blocks * page_size >= budget; disjoint from the pages of the batch).  Weights are >= 0
+ * (others rank by the order of their bits, NaN included).
+ *   kept_out_dev     int32 [n_seqs][per_head ? n_kv_heads : 1][budget]: kept rows ascending, then -1
+ *   new_len_out_dev  int32 [n_seqs]: min(kv_len, budget); may be kv_len_dev itself
+ * q_start_dev is not read (may be NULL).  n_sink + n_recent <= budget (ILRE_ERR_BUDGET).
+ */
+int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t budget, int32_t n_sink,
+                     int32_t n_recent, int32_t per_head, const ilre_paged_pool_t* pool,
+                     const int32_t* dst_table_dev, int32_t dst_blocks, int32_t* kept_out_dev,
+                     int32_t* new_len_out_dev, void* cuda_stream);
+
+/* As ilre_recall_status, _last_launch_count, _check_guards and _destroy. */
+int ilre_paged_status(ilre_paged_t* h);
+int ilre_paged_last_launch_count(ilre_paged_t* h);
+int ilre_paged_check_guards(ilre_paged_t* h);
+int ilre_paged_destroy(ilre_paged_t* h);
 
 const char* ilre_strerror(int code);
 

@@ -8,9 +8,8 @@
 #include <cstring>
 #include <new>
 
-#include <nvtx3/nvToolsExt.h>
-
 #include "../../include/ilre_recall.h"
+#include "api_common.cuh"
 #include "attn_kernels.cuh"
 #include "fill_kernels.cuh"
 #include "qk_geometry.cuh"
@@ -24,11 +23,6 @@ using namespace ilre;
 
 namespace {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 constexpr int kNumStages = 4;            // timed stages (see ilre_recall_stage_times)
 constexpr int kProfRing = 32;            // runs whose stage events are kept for averaging
 constexpr int kMaxSinkStaging = 65536;
@@ -36,10 +30,6 @@ static constexpr int kHostPieces = 16;              // most pieces of a pipeline
 static constexpr long long kHostPieceMinKeys = 65536;   // no piece shorter than this (128-key multiple)
 
 }  // namespace
-
-static constexpr int kGuardBytes = 256;       // written once behind every workspace buffer
-static constexpr int kGuardByte = 0xA5;
-static constexpr int kMaxGuards = 48;
 
 struct ilre_recall {
   ilre_recall_config_t cfg;
@@ -103,14 +93,6 @@ struct ilre_recall {
 
 namespace {
 
-// A named range on the host time line for tracing tools that read NVTX (a no-op without one).
-struct TraceRange {
-  explicit TraceRange(const char* name) { nvtxRangePushA(name); }
-  ~TraceRange() { nvtxRangePop(); }
-  TraceRange(const TraceRange&) = delete;
-  TraceRange& operator=(const TraceRange&) = delete;
-};
-
 // True while `st` is being captured into a CUDA graph.
 bool capturing(cudaStream_t st) {
   cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
@@ -123,30 +105,6 @@ bool capturing(cudaStream_t st) {
 cudaError_t wait_for_tables(cudaStream_t st, cudaEvent_t ev) {
   if (capturing(st)) return cudaSuccess;
   return cudaStreamWaitEvent(st, ev, 0);
-}
-
-struct DeviceGuard {
-  int prev;
-  bool ok;
-  explicit DeviceGuard(int dev) : prev(-1), ok(false) {
-    if (cudaGetDevice(&prev) != cudaSuccess) return;
-    ok = (prev == dev) || (cudaSetDevice(dev) == cudaSuccess);
-  }
-  ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
-
-// One workspace buffer of the handle, followed by a guard zone of kGuardBytes that nothing may
-// write to (checked by ilre_recall_check_guards).
-template <class T>
-bool dev_alloc(ilre_recall* h, T** p, size_t count) {
-  *p = nullptr;
-  const size_t bytes = ((count ? count : 1) * sizeof(T) + 15) & ~static_cast<size_t>(15);
-  if (h->n_guards >= kMaxGuards) return false;
-  if (cudaMalloc(reinterpret_cast<void**>(p), bytes + kGuardBytes) != cudaSuccess) return false;
-  uint8_t* zone = reinterpret_cast<uint8_t*>(*p) + bytes;
-  if (cudaMemset(zone, kGuardByte, kGuardBytes) != cudaSuccess) return false;
-  h->guard[h->n_guards++] = zone;
-  return true;
 }
 
 void free_all(ilre_recall* h) {
@@ -221,11 +179,6 @@ int validate_run(const ilre_recall* h, const void* k, long long L, const void* q
   return ILRE_OK;
 }
 
-#define ILRE_CUDA(expr)                                   \
-  do {                                                    \
-    if ((expr) != cudaSuccess) return ILRE_ERR_CUDA;      \
-  } while (0)
-
 }  // namespace
 
 extern "C" {
@@ -258,14 +211,11 @@ int ilre_recall_create(const ilre_recall_config_t* cfg, ilre_recall_t** out) {
   h->n_sm = prop.multiProcessorCount;
   h->wait_limit = kWaitCycleLimit;
 
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) !=
-          cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
+  h->encode = tensor_map_encoder();
+  if (!h->encode) {
     delete h;
     return ILRE_ERR_CUDA;
   }
-  h->encode = reinterpret_cast<EncodeTiledFn>(fn);
 
   const int group_size = cfg->n_q_heads / cfg->n_kv_heads;
   const size_t rows_pad = static_cast<size_t>(rows_padded_bound(group_size, cfg->max_q_len));
@@ -845,16 +795,7 @@ int ilre_recall_check_guards(ilre_recall_t* h) {
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   if (cudaDeviceSynchronize() != cudaSuccess) return ILRE_ERR_CUDA;
-  int damaged = 0;
-  uint8_t zone[kGuardBytes];
-  for (int i = 0; i < h->n_guards; ++i) {
-    if (cudaMemcpy(zone, h->guard[i], kGuardBytes, cudaMemcpyDeviceToHost) != cudaSuccess)
-      return ILRE_ERR_CUDA;
-    bool intact = true;
-    for (int b = 0; b < kGuardBytes; ++b) intact = intact && zone[b] == kGuardByte;
-    damaged += intact ? 0 : 1;
-  }
-  return damaged;
+  return damaged_guards(h->guard, h->n_guards);
 }
 
 int ilre_recall_last_launch_count(ilre_recall_t* h) {
@@ -883,6 +824,7 @@ const char* ilre_strerror(int code) {
     case ILRE_ERR_DEVICE_WAIT: return "a bounded wait inside a kernel gave up";
     case ILRE_ERR_QUOTA: return "a combination ran out of candidates";
     case ILRE_ERR_NOMEM: return "device allocation failed";
+    case ILRE_ERR_BATCH: return "lengths or page numbers of a batch out of range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,373 @@
+// C ABI of the paged cache: handle, argument validation, launches; and the rotary positions without a handle.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+
+#include "../../include/ilre_recall.h"
+#include "api_common.cuh"
+#include "launch.cuh"
+#include "paged_attn_kernels.cuh"
+#include "paged_weight_kernels.cuh"
+#include "rope_kernels.cuh"
+#include "sm100_ptx.cuh"
+
+using namespace ilre;
+
+struct ilre_paged {
+  ilre_paged_config_t cfg;
+  int n_sm;
+  EncodeTiledFn encode;
+  const uint8_t* guard[kMaxGuards];
+  int n_guards;
+  float* part_o;                        // partial results of cut items
+  float2* part_ml;
+  uint32_t* arrived;
+  int32_t* n_keep;                      // rows that an eviction keeps of each sequence
+  int* status;
+  int last_launches;
+  cudaStream_t last_stream;
+};
+
+namespace {
+
+constexpr int kDim = 128;
+constexpr double kPi = 3.14159265358979323846;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+void free_all(ilre_paged* h) {
+  cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->status);
+}
+
+// Full turns per position of every channel pair.
+int make_freqs(const ilre_rope_spec_t* s, int head_dim, RopeFreqs* f) {
+  std::memset(f, 0, sizeof(*f));
+  if (!s) return ILRE_OK;                                // nothing turns
+  if (!(s->theta > 1.0) || !std::isfinite(s->theta) || s->rotary_dim < 1 || s->layout < ILRE_ROPE_HALF ||
+      s->layout > ILRE_ROPE_INTERLEAVED || s->scaling < ILRE_ROPE_PLAIN || s->scaling > ILRE_ROPE_YARN ||
+      !(s->attn_factor >= 0.0) || !std::isfinite(s->attn_factor))
+    return ILRE_ERR_INVALID_ARG;
+  if (s->scaling != ILRE_ROPE_PLAIN && (!(s->factor >= 1.0) || !std::isfinite(s->factor))) return ILRE_ERR_INVALID_ARG;
+  if (s->scaling >= ILRE_ROPE_BANDED &&
+      (!(s->orig_len >= 1.0) || !std::isfinite(s->orig_len) || !(s->low > 0.0) || !(s->high > s->low) ||
+       !std::isfinite(s->high)))
+    return ILRE_ERR_INVALID_ARG;
+  if (s->rotary_dim % 16 != 0 || s->rotary_dim > head_dim || s->rotary_dim > 2 * kRopeMaxPairs)
+    return ILRE_ERR_UNSUPPORTED;
+  const int R = s->rotary_dim;
+  double lo = 0.0, hi = 0.0;
+  if (s->scaling == ILRE_ROPE_YARN) {
+    const auto d = [&](double n) { return R * std::log(s->orig_len / (2.0 * kPi * n)) / (2.0 * std::log(s->theta)); };
+    lo = std::fmax(std::floor(d(s->high)), 0.0);
+    hi = std::fmin(std::ceil(d(s->low)), R - 1.0);
+  }
+  for (int i = 0; i < R / 2; ++i) {
+    const double b = std::pow(s->theta, -2.0 * i / R);
+    double x = b;
+    if (s->scaling == ILRE_ROPE_LINEAR) x = b / s->factor;
+    if (s->scaling == ILRE_ROPE_BANDED) {
+      const double t = std::fmin(1.0, std::fmax(0.0, (s->orig_len * b / (2.0 * kPi) - s->low) / (s->high - s->low)));
+      x = (1.0 - t) * b / s->factor + t * b;
+    }
+    if (s->scaling == ILRE_ROPE_YARN) {
+      const double r = std::fmin(1.0, std::fmax(0.0, (i - lo) / std::fmax(hi - lo, 0.001)));
+      x = r * b / s->factor + (1.0 - r) * b;
+    }
+    f->turns[i] = x / (2.0 * kPi);
+  }
+  const double own = s->scaling == ILRE_ROPE_YARN ? 0.1 * std::log(s->factor) + 1.0 : 1.0;
+  f->scale = static_cast<float>(s->attn_factor > 0.0 ? s->attn_factor : own);
+  f->rotary_dim = R;
+  f->interleaved = s->layout == ILRE_ROPE_INTERLEAVED;
+  return ILRE_OK;
+}
+
+// The batch's and the pool's numbers and pointers; fills the kernels' form.  with_q: q_start is read.
+int validate_batch(const ilre_paged* h, const ilre_paged_batch_t* b, const ilre_paged_pool_t* pool, bool with_q,
+                   PagedBatch* out) {
+  if (!h || !b || !pool) return ILRE_ERR_INVALID_ARG;
+  if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_q_len < 0 || b->max_blocks < 0 || pool->n_pages < 0)
+    return ILRE_ERR_INVALID_ARG;
+  if (b->n_seqs > 0 && ((with_q && !b->q_start_dev) || !b->kv_len_dev || (b->max_blocks > 0 && !b->block_table_dev)))
+    return ILRE_ERR_INVALID_ARG;
+  if (b->n_seqs > h->cfg.max_seqs ||
+      static_cast<long long>(b->max_blocks) * h->cfg.page_size >= 2147483647LL - 2048)
+    return ILRE_ERR_CAPACITY;
+  int shift = 0;
+  while ((1 << shift) < h->cfg.page_size) ++shift;
+  *out = PagedBatch{b->n_seqs, b->n_tokens, b->max_q_len, b->max_blocks, shift, pool->n_pages, b->q_start_dev,
+                    b->kv_len_dev, b->block_table_dev, h->status};
+  return ILRE_OK;
+}
+
+int validate_pool(const ilre_paged* h, const void* base, int64_t* stride) {
+  if (!base) return ILRE_ERR_INVALID_ARG;
+  const int64_t least = static_cast<int64_t>(h->cfg.page_size) * h->cfg.n_kv_heads * kDim;
+  if (*stride == 0) *stride = least;
+  if (*stride < least || *stride > (1ll << 38)) return ILRE_ERR_INVALID_ARG;
+  if (!aligned16(base) || *stride % 8 != 0) return ILRE_ERR_ALIGNMENT;
+  return ILRE_OK;
+}
+
+// Rows of `heads` heads with `stride` elements from token to token.
+int validate_rows(const void* base, int64_t stride, int64_t heads, int head_dim) {
+  if (!base || stride < heads * head_dim || stride > (1ll << 38)) return ILRE_ERR_INVALID_ARG;
+  if (!aligned16(base) || stride % 8 != 0) return ILRE_ERR_ALIGNMENT;
+  return ILRE_OK;
+}
+
+// A pool as {channel, kv head, row of the page, page}, boxes of 64 channels of one head by box_rows rows.
+bool encode_pool(const ilre_paged* h, CUtensorMap* map, const void* base, int64_t page_stride, int n_pages,
+                 int box_rows) {
+  const cuuint64_t n_kv = h->cfg.n_kv_heads, ps = h->cfg.page_size;
+  const cuuint64_t gdim[4] = {kDim, n_kv, ps, static_cast<cuuint64_t>(n_pages)};
+  const cuuint64_t gstride[3] = {kDim * 2, n_kv * kDim * 2, static_cast<cuuint64_t>(page_stride) * 2};
+  const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(box_rows), 1};
+  const cuuint32_t estride[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType t = h->cfg.dtype == ILRE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return h->encode(map, t, 4, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+float softmax_scale() { return static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kDim))); }
+
+#define ILRE_CHECK(expr)                \
+  do {                                  \
+    const int rc_ = (expr);             \
+    if (rc_ != ILRE_OK) return rc_;     \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride, void* out_dev, int64_t out_stride,
+              const int32_t* pos_dev, int64_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t dtype,
+              int32_t transposed, void* cuda_stream) {
+  TraceRange trace("ilre: rotary positions (Eq. 3)");
+  if (!spec || n_tokens < 0 || n_heads < 1 || head_dim < 1 || dtype < ILRE_BF16 || dtype > ILRE_F16)
+    return ILRE_ERR_INVALID_ARG;
+  if (head_dim % 16 != 0 || head_dim > 1024) return ILRE_ERR_UNSUPPORTED;
+  if (n_heads > 65535 || n_tokens > 2147483647LL) return ILRE_ERR_CAPACITY;
+  RopeFreqs f;
+  ILRE_CHECK(make_freqs(spec, head_dim, &f));
+  if (n_tokens == 0) return ILRE_OK;
+  if (!pos_dev) return ILRE_ERR_INVALID_ARG;
+  ILRE_CHECK(validate_rows(x_dev, x_stride, n_heads, head_dim));
+  ILRE_CHECK(validate_rows(out_dev, out_stride, n_heads, head_dim));
+  int dev = 0, n_sm = 0;
+  ILRE_CUDA(cudaGetDevice(&dev));
+  ILRE_CUDA(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
+  RopeParams p;
+  p.rows = RopeRows{x_dev, out_dev, x_stride, out_stride, n_heads};
+  p.pos = pos_dev; p.n_tokens = n_tokens; p.head_dim = head_dim;
+  p.sign = transposed ? -1.f : 1.f;
+  ILRE_CUDA(launch_rope(f, p, dtype == ILRE_F16, n_sm, static_cast<cudaStream_t>(cuda_stream)));
+  return ILRE_OK;
+}
+
+int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
+  if (!cfg || !out) return ILRE_ERR_INVALID_ARG;
+  if (cfg->n_kv_heads < 1 || cfg->n_q_heads < 1 || cfg->max_seqs < 1 || cfg->device < 0 || cfg->dtype < ILRE_BF16 ||
+      cfg->dtype > ILRE_F16 || cfg->page_size < 1)
+    return ILRE_ERR_INVALID_ARG;
+  if (cfg->head_dim != kDim || cfg->n_q_heads % cfg->n_kv_heads != 0 || cfg->n_q_heads / cfg->n_kv_heads > 128 ||
+      cfg->page_size < 16 || cfg->page_size > 1024 || (cfg->page_size & (cfg->page_size - 1)) != 0)
+    return ILRE_ERR_UNSUPPORTED;
+  if (cfg->max_seqs > 65535 || cfg->n_kv_heads > 1024) return ILRE_ERR_CAPACITY;
+  int n_dev = 0;
+  if (cudaGetDeviceCount(&n_dev) != cudaSuccess || cfg->device >= n_dev) return ILRE_ERR_CUDA;
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaDeviceProp prop;
+  ILRE_CUDA(cudaGetDeviceProperties(&prop, cfg->device));
+  if (prop.major != 10) return ILRE_ERR_UNSUPPORTED;
+  ilre_paged* h = new (std::nothrow) ilre_paged();
+  if (!h) return ILRE_ERR_NOMEM;
+  std::memset(h, 0, sizeof(*h));
+  h->cfg = *cfg;
+  h->n_sm = prop.multiProcessorCount;
+  h->encode = tensor_map_encoder();
+  if (!h->encode) {
+    delete h;
+    return ILRE_ERR_CUDA;
+  }
+  const size_t ctas = static_cast<size_t>(h->n_sm) * kRowCtasPerSm;
+  bool ok = dev_alloc(h, &h->part_o, ctas * 2 * kRowTile * kDim);
+  ok = ok && dev_alloc(h, &h->part_ml, ctas * 2 * kRowTile);
+  ok = ok && dev_alloc(h, &h->arrived, ctas);
+  ok = ok && dev_alloc(h, &h->n_keep, cfg->max_seqs);
+  ok = ok && dev_alloc(h, &h->status, 1);
+  if (ok) ok = cudaMemset(h->status, 0, sizeof(int)) == cudaSuccess;
+  if (ok) ok = cudaMemset(h->arrived, 0, ctas * sizeof(uint32_t)) == cudaSuccess;
+  if (ok) ok = cudaDeviceSynchronize() == cudaSuccess;
+  if (!ok) {
+    cudaGetLastError();
+    free_all(h);
+    delete h;
+    return ILRE_ERR_NOMEM;
+  }
+  *out = h;
+  return ILRE_OK;
+}
+
+int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const ilre_rope_spec_t* spec,
+                      const int32_t* pos_dev, const void* q_dev, int64_t q_stride, void* q_out_dev,
+                      int64_t q_out_stride, const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                      const ilre_paged_pool_t* pool, void* cuda_stream) {
+  TraceRange trace("ilre: new rows of the paged cache");
+  AppendParams p;
+  std::memset(&p, 0, sizeof(p));
+  ILRE_CHECK(validate_batch(h, batch, pool, true, &p.batch));
+  RopeFreqs f;
+  ILRE_CHECK(make_freqs(spec, kDim, &f));
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return ILRE_OK;
+  if ((spec && !pos_dev) || (q_dev == nullptr) != (q_out_dev == nullptr)) return ILRE_ERR_INVALID_ARG;
+  int64_t ks = pool->k_page_stride, vs = pool->v_page_stride;
+  ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
+  ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));
+  ILRE_CHECK(validate_rows(k_dev, k_stride, h->cfg.n_kv_heads, kDim));
+  ILRE_CHECK(validate_rows(v_dev, v_stride, h->cfg.n_kv_heads, kDim));
+  if (q_dev) {
+    ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
+    ILRE_CHECK(validate_rows(q_out_dev, q_out_stride, h->cfg.n_q_heads, kDim));
+  }
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_stream = st;
+  p.q = RopeRows{q_dev, q_out_dev, q_stride, q_out_stride, q_dev ? h->cfg.n_q_heads : 0};
+  p.k = RopeRows{k_dev, pool->k_dev, k_stride, 0, h->cfg.n_kv_heads};
+  p.v = RopeRows{v_dev, pool->v_dev, v_stride, 0, h->cfg.n_kv_heads};
+  p.k_page_stride = ks; p.v_page_stride = vs;
+  p.w = pool->w_dev; p.pos = pos_dev; p.n_kv = h->cfg.n_kv_heads;
+  ILRE_CUDA(launch_append(f, p, h->cfg.dtype == ILRE_F16, h->n_sm, st));
+  h->last_launches = 1;
+  return ILRE_OK;
+}
+
+int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev, int64_t q_stride,
+                         const ilre_paged_pool_t* pool, void* out_dev, float* lse_out_dev, void* cuda_stream) {
+  TraceRange trace("ilre: attention over the paged cache");
+  PagedAttnParams p;
+  std::memset(&p, 0, sizeof(p));
+  ILRE_CHECK(validate_batch(h, batch, pool, true, &p.batch));
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return ILRE_OK;
+  if (pool->n_pages < 1) return ILRE_ERR_INVALID_ARG;
+  int64_t ks = pool->k_page_stride, vs = pool->v_page_stride;
+  ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
+  ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));
+  ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
+  if (!out_dev) return ILRE_ERR_INVALID_ARG;
+  if (!aligned16(out_dev)) return ILRE_ERR_ALIGNMENT;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_stream = st;
+  p.q = q_dev; p.q_stride = q_stride; p.out = out_dev; p.lse = lse_out_dev;
+  p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
+  p.c2 = softmax_scale();
+  p.part_o = h->part_o; p.part_ml = h->part_ml; p.arrived = h->arrived;
+  CUtensorMap map_k, map_v;
+  const int box = h->cfg.page_size < kRowKeys ? h->cfg.page_size : kRowKeys;
+  if (!encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, box) ||
+      !encode_pool(h, &map_v, pool->v_dev, vs, pool->n_pages, box))
+    return ILRE_ERR_CUDA;
+  ILRE_CUDA(launch_paged_rows(map_k, map_v, p, h->cfg.dtype == ILRE_F16, h->n_sm, st));
+  h->last_launches = 1;
+  return ILRE_OK;
+}
+
+int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev, int64_t q_stride,
+                          const float* lse_dev, const ilre_paged_pool_t* pool, void* cuda_stream) {
+  TraceRange trace("ilre: accumulated attention weight");
+  PagedWeightParams p;
+  std::memset(&p, 0, sizeof(p));
+  ILRE_CHECK(validate_batch(h, batch, pool, true, &p.batch));
+  if (batch->n_tokens == 0 || batch->n_seqs == 0 || batch->max_blocks == 0) return ILRE_OK;
+  if (pool->n_pages < 1 || !lse_dev || !pool->w_dev) return ILRE_ERR_INVALID_ARG;
+  int64_t ks = pool->k_page_stride;
+  ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
+  ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_stream = st;
+  p.q = q_dev; p.q_stride = q_stride; p.k = pool->k_dev; p.k_page_stride = ks;
+  p.lse = lse_dev; p.w = pool->w_dev;
+  p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
+  p.c2 = softmax_scale();
+  ILRE_CUDA(launch_paged_weights(p, h->cfg.dtype == ILRE_F16, st));
+  h->last_launches = 1;
+  return ILRE_OK;
+}
+
+int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t budget, int32_t n_sink,
+                     int32_t n_recent, int32_t per_head, const ilre_paged_pool_t* pool, const int32_t* dst_table_dev,
+                     int32_t dst_blocks, int32_t* kept_out_dev, int32_t* new_len_out_dev, void* cuda_stream) {
+  TraceRange trace("ilre: eviction by accumulated weight");
+  EvictParams p;
+  std::memset(&p, 0, sizeof(p));
+  ILRE_CHECK(validate_batch(h, batch, pool, false, &p.batch));
+  if (budget < 1 || n_sink < 0 || n_recent < 0) return ILRE_ERR_INVALID_ARG;
+  if (static_cast<long long>(n_sink) + n_recent > budget) return ILRE_ERR_BUDGET;
+  if (dst_table_dev && (dst_blocks < 1 || static_cast<long long>(dst_blocks) * h->cfg.page_size < budget))
+    return ILRE_ERR_INVALID_ARG;
+  if (batch->n_seqs == 0) return ILRE_OK;
+  if (!pool->w_dev || !kept_out_dev || !new_len_out_dev) return ILRE_ERR_INVALID_ARG;
+  p.k_page_stride = pool->k_page_stride;
+  p.v_page_stride = pool->v_page_stride;
+  int64_t ks = pool->k_page_stride, vs = pool->v_page_stride;
+  ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
+  ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_stream = st;
+  p.k = pool->k_dev; p.v = pool->v_dev; p.w = pool->w_dev; p.k_page_stride = ks; p.v_page_stride = vs;
+  p.n_kv = h->cfg.n_kv_heads; p.budget = budget; p.n_sink = n_sink; p.n_recent = n_recent;
+  p.per_head = per_head != 0; p.dst_table = dst_table_dev; p.dst_blocks = dst_blocks;
+  p.kept = kept_out_dev; p.new_len = new_len_out_dev; p.n_keep = h->n_keep;
+  ILRE_CUDA(launch_evict(p, h->n_sm, st));
+  h->last_launches = 2;
+  return ILRE_OK;
+}
+
+int ilre_paged_status(ilre_paged_t* h) {
+  if (!h) return ILRE_ERR_INVALID_ARG;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  ILRE_CUDA(cudaStreamSynchronize(h->last_stream));
+  int word = 0;
+  ILRE_CUDA(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));
+  if (word == 0) return ILRE_OK;
+  ILRE_CUDA(cudaMemset(h->status, 0, sizeof(int)));
+  return (word == kDevBadLengths || word == kDevBadPage) ? ILRE_ERR_BATCH : ILRE_ERR_DEVICE_WAIT;
+}
+
+int ilre_paged_last_launch_count(ilre_paged_t* h) { return h ? h->last_launches : ILRE_ERR_INVALID_ARG; }
+
+int ilre_paged_check_guards(ilre_paged_t* h) {
+  if (!h) return ILRE_ERR_INVALID_ARG;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  ILRE_CUDA(cudaDeviceSynchronize());
+  return damaged_guards(h->guard, h->n_guards);
+}
+
+int ilre_paged_destroy(ilre_paged_t* h) {
+  if (!h) return ILRE_ERR_INVALID_ARG;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return ILRE_ERR_CUDA;
+  cudaDeviceSynchronize();
+  free_all(h);
+  delete h;
+  return ILRE_OK;
+}
+
+}  // extern "C"

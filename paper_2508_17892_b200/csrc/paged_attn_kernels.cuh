@@ -1,0 +1,33 @@
+// Attention of new tokens over the paged cache.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sm100_ptx.cuh"
+#include "paged_batch.cuh"
+
+namespace ilre {
+
+static constexpr int kRowTile = 16;              // query rows of a work item of the row kernel
+static constexpr int kRowKeys = 64;              // keys of a stage
+static constexpr int kRowCtasPerSm = 2;
+
+struct PagedAttnParams {
+  PagedBatch batch;
+  const void* q;
+  long long q_stride;                            // elements from token to token
+  void* out;                                     // [n_tokens][n_q][128]
+  float* lse;                                    // [n_tokens][n_q] or null
+  int n_q, n_kv, group;
+  float c2;                                      // log2(e) / sqrt(d)
+  float* part_o;                                 // [CTA][2][rows][128]
+  float2* part_ml;                               // [CTA][2][rows]: (maximum in log2 units, sum)
+  uint32_t* arrived;                             // [CTA], 0 between launches
+};
+
+// map_k, map_v: the pools as {channel, kv head, row, page}, boxes of 64 channels x min(page_size, kRowKeys) rows.
+cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v, const PagedAttnParams& p, bool f16,
+                              int n_sm, cudaStream_t st);
+
+}  // namespace ilre

@@ -1,0 +1,323 @@
+"""Python binding of the paged cache in ``include/ilre_recall.h`` (argument marshalling only): what a compressed
+prompt is answered from.
+
+``PagedCache`` appends new rows (with their rotary positions), attends over the cached ones, gathers the attention
+weight that each row receives and evicts by it; ``rope`` turns a tensor of heads alone.  Tensors are the caller's.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+from typing import Optional, Tuple
+
+import torch
+
+from .recall import IlreError, load_library
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_SCALINGS = {"none": 0, "linear": 1, "banded": 2, "yarn": 3}
+
+
+class IlreRopeSpec(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("factor", ctypes.c_double), ("orig_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("attn_factor", ctypes.c_double)]
+
+
+class IlrePagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_kv_heads", "n_q_heads", "head_dim", "page_size", "dtype", "max_seqs",
+                                              "device")]
+
+
+class IlrePagedBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_q_len", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p)]
+
+
+class IlrePagedPool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("w", ctypes.c_void_p),
+                ("k_page_stride", ctypes.c_int64), ("v_page_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32)]
+
+
+def declare(lib: ctypes.CDLL) -> None:
+    """Prototypes of the calls in this module."""
+    vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    spec, batch, pool = (ctypes.POINTER(t) for t in (IlreRopeSpec, IlrePagedBatch, IlrePagedPool))
+    lib.ilre_rope.argtypes = [spec, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp]
+    lib.ilre_paged_create.argtypes = [ctypes.POINTER(IlrePagedConfig), ctypes.POINTER(vp)]
+    lib.ilre_paged_append.argtypes = [vp, batch, spec, vp, vp, i64, vp, i64, vp, i64, vp, i64, pool, vp]
+    lib.ilre_paged_attention.argtypes = [vp, batch, vp, i64, pool, vp, vp, vp]
+    lib.ilre_paged_accumulate.argtypes = [vp, batch, vp, i64, vp, pool, vp]
+    lib.ilre_paged_evict.argtypes = [vp, batch, i32, i32, i32, i32, pool, vp, i32, vp, vp, vp]
+    for name in ("status", "last_launch_count", "check_guards", "destroy"):
+        getattr(lib, "ilre_paged_" + name).argtypes = [vp]
+
+
+@dataclass(frozen=True)
+class RopeSpec:
+    """Rotary positions: layout, rotated part of the head and scaling (see ``ilre_rope_spec_t``).
+
+    scaling: "none", "linear", "banded" (low, high: frequency factors) or "yarn" (low, high: the turns
+    beta_slow, beta_fast).  attn_factor 0: 0.1 ln(factor) + 1 with "yarn", else 1."""
+    theta: float = 500000.0
+    rotary_dim: int = 128
+    interleaved: bool = False
+    scaling: str = "none"
+    factor: float = 1.0
+    orig_len: float = 8192
+    low: float = 1.0
+    high: float = 4.0
+    attn_factor: float = 0.0
+
+    def c_struct(self) -> IlreRopeSpec:
+        return IlreRopeSpec(self.theta, self.rotary_dim, int(self.interleaved), _SCALINGS[self.scaling], self.factor,
+                            self.orig_len, self.low, self.high, self.attn_factor)
+
+
+@dataclass(frozen=True)
+class PagedBatch:
+    """Sequences of one call (``ilre_paged_batch_t``); keeps its tensors alive."""
+    q_start: Optional[torch.Tensor]
+    kv_len: torch.Tensor
+    block_table: torch.Tensor
+    n_tokens: int
+    max_q_len: int
+
+    def c_struct(self) -> IlrePagedBatch:
+        return IlrePagedBatch(self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1],
+                              self.q_start.data_ptr() if self.q_start is not None else None, self.kv_len.data_ptr(),
+                              self.block_table.data_ptr())
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return t.data_ptr() if t is not None else None
+
+
+def _rows(t: torch.Tensor, device, dtype, heads: int, dim: int) -> int:
+    """Stride in elements from token to token of a tensor [n, heads, dim] whose tokens are contiguous."""
+    assert t.device == device and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, dim)
+    assert t.shape[0] == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim))
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+class _OnStream:
+    """The stream of a call: its device is current inside, tensors made inside are its own, and the caller's
+    tensors are marked as in use by it."""
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], tensors):
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        if stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        self._ctx = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self._ctx.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        return self._ctx.__exit__(*exc)
+
+
+def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: bool = False,
+         out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """x [n_tokens, n_heads, head_dim] (bf16 or fp16; tokens may be strided) turned by int32 ``positions``.
+
+    ``out`` may be ``x``.  ``transposed`` applies the transposed map: the gradient of ``rope`` with
+    respect to x is ``rope(grad, positions, spec, transposed=True)``."""
+    assert x.is_cuda and x.dtype in _DTYPES and x.dim() == 3
+    n, heads, dim = x.shape
+    assert positions.device == x.device and positions.dtype == torch.int32 and positions.is_contiguous()
+    assert positions.shape == (n,)
+    x_stride = _rows(x, x.device, x.dtype, heads, dim)
+    with _OnStream(x.device, stream, (x, positions, out)) as st:
+        if out is None:
+            out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
+        out_stride = _rows(out, x.device, x.dtype, heads, dim)
+        assert out.shape[0] == n
+        rc = load_library().ilre_rope(ctypes.byref(spec.c_struct()), x.data_ptr(), x_stride, out.data_ptr(), out_stride,
+                                      positions.data_ptr(), n, heads, dim, _DTYPES[x.dtype], int(transposed), st)
+    if rc != 0:
+        raise IlreError(rc, "ilre_rope")
+    return out
+
+
+class PagedCache:
+    """Owns one ``ilre_paged_t`` handle; the pools, tables and lengths are the caller's tensors.
+
+    k_pool, v_pool: [n_pages, page_size, n_kv_heads, 128], pages contiguous (the stride from page to page is
+    free, so the two may be halves of one tensor); w_pool: fp32 [n_pages, n_kv_heads, page_size].
+    One stream at a time; graphs that hold calls of one handle must not run at the same time."""
+
+    def __init__(self, n_kv_heads: int = 8, n_q_heads: int = 32, page_size: int = 64,
+                 dtype: torch.dtype = torch.bfloat16, max_seqs: int = 256, head_dim: int = 128, device: int = 0):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        self.cfg = IlrePagedConfig(n_kv_heads, n_q_heads, head_dim, page_size, _DTYPES[dtype], max_seqs, device)
+        rc = self._lib.ilre_paged_create(ctypes.byref(self.cfg), ctypes.byref(self._h))
+        if rc != 0:
+            self._h = ctypes.c_void_p()
+            raise IlreError(rc, "ilre_paged_create")
+        self.dtype = dtype
+        self.device = torch.device("cuda", device)
+
+    def batch(self, q_start: Optional[torch.Tensor], kv_len: torch.Tensor, block_table: torch.Tensor, n_tokens: int,
+              max_q_len: int) -> PagedBatch:
+        """q_start int32 [n_seqs + 1] (None for ``evict``), kv_len int32 [n_seqs] (the new tokens' rows among
+        them), block_table int32 [n_seqs, max_blocks]; at most max_q_len new tokens per sequence."""
+        for t in (q_start, kv_len, block_table):
+            assert t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous())
+        assert kv_len.dim() == 1 and block_table.dim() == 2 and block_table.shape[0] == kv_len.numel()
+        assert q_start is None or q_start.shape == (kv_len.numel() + 1,)
+        return PagedBatch(q_start, kv_len, block_table, n_tokens, max_q_len)
+
+    def _pool(self, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
+        c = self.cfg
+        for t in (k, v):
+            assert t is None or (t.device == self.device and t.dtype == self.dtype and t.dim() == 4 and
+                                 t.shape == (k.shape[0], c.page_size, c.n_kv_heads, c.head_dim) and
+                                 (t.shape[0] == 0 or t[0].is_contiguous()))
+        assert w is None or (w.device == self.device and w.dtype == torch.float32 and w.is_contiguous() and
+                             w.shape == (k.shape[0], c.n_kv_heads, c.page_size))
+        stride = lambda t: t.stride(0) if t is not None and t.shape[0] > 1 else 0  # noqa: E731
+        return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), stride(k), stride(v), k.shape[0])
+
+    def _q(self, batch: PagedBatch, q: torch.Tensor) -> int:
+        assert q.shape[0] == batch.n_tokens and (batch.n_tokens == 0 or batch.q_start is not None)
+        return _rows(q, self.device, self.dtype, self.cfg.n_q_heads, self.cfg.head_dim)
+
+    def _check(self, rc: int, what: str) -> None:
+        if rc != 0:
+            raise IlreError(rc, what)
+
+    def append(self, batch: PagedBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+               positions: Optional[torch.Tensor], spec: Optional[RopeSpec], k_pool: torch.Tensor, v_pool: torch.Tensor,
+               w_pool: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+        """k turned and v copied to the new tokens' rows, their weights cleared; returns q turned (``q_out``, which
+        may be q; made here if not given).  spec None: nothing is turned."""
+        c = self.cfg
+        n = batch.n_tokens
+        assert k.shape[0] == n and v.shape[0] == n
+        k_stride, v_stride = (_rows(t, self.device, self.dtype, c.n_kv_heads, c.head_dim) for t in (k, v))
+        if spec is not None:
+            assert positions is not None
+        if positions is not None:
+            assert positions.device == self.device and positions.dtype == torch.int32 and positions.is_contiguous()
+            assert positions.shape == (n,)
+        pool = self._pool(k_pool, v_pool, w_pool)
+        with _OnStream(self.device, stream, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start,
+                                             batch.kv_len, batch.block_table)) as st:
+            q_stride = q_out_stride = 0
+            if q is not None:
+                q_stride = self._q(batch, q)
+                if q_out is None:
+                    q_out = torch.empty(n, c.n_q_heads, c.head_dim, dtype=q.dtype, device=q.device)
+                q_out_stride = self._q(batch, q_out)
+            else:
+                assert q_out is None
+            self._check(self._lib.ilre_paged_append(
+                self._h, ctypes.byref(batch.c_struct()), ctypes.byref(spec.c_struct()) if spec is not None else None,
+                _ptr(positions), _ptr(q), q_stride, _ptr(q_out), q_out_stride, k.data_ptr(), k_stride, v.data_ptr(),
+                v_stride, ctypes.byref(pool), st), "ilre_paged_append")
+        return q_out
+
+    def attention(self, batch: PagedBatch, q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        """Every new token over its sequence's cached rows up to itself: (out like q, lse fp32 [n_tokens, n_q_heads]
+        or None).  Rows of tokens that belong to no sequence are left as they are."""
+        c = self.cfg
+        q_stride = self._q(batch, q)
+        pool = self._pool(k_pool, v_pool, None)
+        with _OnStream(self.device, stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len,
+                                             batch.block_table)) as st:
+            if out is None:
+                out = torch.empty(batch.n_tokens, c.n_q_heads, c.head_dim, dtype=q.dtype, device=q.device)
+            if lse is None and want_lse:
+                lse = torch.empty(batch.n_tokens, c.n_q_heads, dtype=torch.float32, device=q.device)
+            assert out.device == self.device and out.dtype == self.dtype and out.is_contiguous()
+            assert out.shape == (batch.n_tokens, c.n_q_heads, c.head_dim)
+            self._lse(batch, lse)
+            self._check(self._lib.ilre_paged_attention(
+                self._h, ctypes.byref(batch.c_struct()), q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
+                _ptr(lse), st), "ilre_paged_attention")
+        return out, lse
+
+    def _lse(self, batch: PagedBatch, lse: Optional[torch.Tensor]) -> None:
+        assert lse is None or (lse.device == self.device and lse.dtype == torch.float32 and lse.is_contiguous() and
+                               lse.shape == (batch.n_tokens, self.cfg.n_q_heads))
+
+    def accumulate(self, batch: PagedBatch, q: torch.Tensor, lse: torch.Tensor, k_pool: torch.Tensor,
+                   w_pool: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Adds to w_pool the attention weight that every cached row received from the batch's new tokens (q and lse
+        as ``attention`` had and returned them).  Returns w_pool."""
+        q_stride = self._q(batch, q)
+        assert lse is not None and w_pool is not None
+        self._lse(batch, lse)
+        pool = self._pool(k_pool, None, w_pool)
+        with _OnStream(self.device, stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len,
+                                             batch.block_table)) as st:
+            self._check(self._lib.ilre_paged_accumulate(
+                self._h, ctypes.byref(batch.c_struct()), q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
+                st), "ilre_paged_accumulate")
+        return w_pool
+
+    def evict(self, batch: PagedBatch, budget: int, n_sink: int, n_recent: int, k_pool: torch.Tensor,
+              v_pool: torch.Tensor, w_pool: torch.Tensor, per_head: bool = False,
+              dst_table: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+              new_len: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """Cuts every sequence to ``budget`` rows: its first n_sink, its last n_recent and the heaviest between them,
+        moved to rows 0, 1, ... of its own pages or of dst_table's (int32 [n_seqs, dst_blocks]).  Returns (kept
+        int32 [n_seqs, n_kv_heads or 1, budget], ascending, -1 behind a shorter sequence; new_len int32 [n_seqs],
+        which may be batch.kv_len)."""
+        n = batch.kv_len.numel()
+        shape = (n, self.cfg.n_kv_heads if per_head else 1, budget)
+        assert budget >= 1 and w_pool is not None
+        pool = self._pool(k_pool, v_pool, w_pool)
+        if dst_table is not None:
+            assert dst_table.device == self.device and dst_table.dtype == torch.int32 and dst_table.is_contiguous()
+            assert dst_table.dim() == 2 and dst_table.shape[0] == n
+        with _OnStream(self.device, stream, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len,
+                                             batch.block_table)) as st:
+            if kept is None:
+                kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+            if new_len is None:
+                new_len = torch.empty(n, dtype=torch.int32, device=self.device)
+            for t, want in ((kept, shape), (new_len, (n,))):
+                assert t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and t.shape == want
+            self._check(self._lib.ilre_paged_evict(
+                self._h, ctypes.byref(batch.c_struct()), budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
+                _ptr(dst_table), dst_table.shape[1] if dst_table is not None else 0, kept.data_ptr(),
+                new_len.data_ptr(), st), "ilre_paged_evict")
+        return kept, new_len
+
+    # -- diagnostics -------------------------------------------------------------------
+    def status(self) -> int:
+        return self._lib.ilre_paged_status(self._h)
+
+    def check_status(self) -> None:
+        self._check(self.status(), "ilre_paged_status")
+
+    def check_guards(self) -> int:
+        """Number of workspace buffers whose guard zone was written to (0 = none); synchronises."""
+        rc = self._lib.ilre_paged_check_guards(self._h)
+        if rc < 0:
+            raise IlreError(rc, "ilre_paged_check_guards")
+        return rc
+
+    def last_launch_count(self) -> int:
+        return self._lib.ilre_paged_last_launch_count(self._h)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.ilre_paged_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

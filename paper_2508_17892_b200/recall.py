@@ -28,6 +28,9 @@ EXPORTED_SYMBOLS = (
     "ilre_recall_sm_clock",
     "ilre_recall_last_launch_count", "ilre_recall_check_guards", "ilre_recall_destroy", "ilre_strerror",
     "ilre_topk_positions_noalloc",
+    "ilre_rope", "ilre_paged_create", "ilre_paged_append", "ilre_paged_attention", "ilre_paged_accumulate",
+    "ilre_paged_evict", "ilre_paged_status", "ilre_paged_last_launch_count", "ilre_paged_check_guards",
+    "ilre_paged_destroy",
 )
 
 NOALLOC_MAX_L = 1048576
@@ -91,6 +94,8 @@ def load_library() -> ctypes.CDLL:
     lib.ilre_strerror.argtypes = [ctypes.c_int]
     lib.ilre_topk_positions_noalloc.argtypes = [vp, i64, i32, vp, vp]
     lib.ilre_strerror.restype = ctypes.c_char_p
+    from .paged import declare
+    declare(lib)
     for name in EXPORTED_SYMBOLS:
         if name != "ilre_strerror":
             getattr(lib, name).restype = ctypes.c_int

@@ -1,0 +1,127 @@
+"""How the paged kernels split a batch: the header's arithmetic, compiled with the host compiler and
+checked against counting.  No GPU."""
+import os
+import subprocess
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2508_17892_b200", "csrc")
+CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+
+BODY = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <vector>
+#include "paged_batch.cuh"
+using namespace ilre;
+static int bad = 0;
+#define CHECK(c) do { if (!(c) && bad++ < 10) std::printf("line %d: %s\n", __LINE__, #c); } while (0)
+
+int main() {
+  std::mt19937 rng(7);
+  auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
+  for (int i = 0; i < 20000; ++i) {
+    const long long n = pick(0, 40), m = pick(1, 130), a = pick(0, 300), b = pick(0, 3000);
+    long long want = 0;
+    for (long long j = 0; j < n; ++j) want += (a * j + b) / m;
+    CHECK(floor_sum(n, m, a, b) == want);
+  }
+  // one head: units, their prefix sums and the tile of each unit
+  const int tqs[] = {1, 2, 4, 16, 36, 64, 256}, tks[] = {64, 128};
+  for (int i = 0; i < 4000; ++i) {
+    HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2]};
+    long long at = 0;
+    for (int qt = 0; qt < h.n_qt(); ++qt) {
+      const int last = std::min((qt + 1) * h.tq, h.n), seen = h.kv - h.n + last;
+      CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + h.tk - 1) / h.tk));
+      CHECK(h.before(qt) == at);
+      for (long long u = at; u < at + h.key_tiles(qt); u += 3) CHECK(h.tile_of(u) == qt);
+      at += h.key_tiles(qt);
+    }
+    CHECK(h.units() == at);
+  }
+  // far lengths: no overflow
+  HeadTiles far{1 << 30, 2147481000, 64, 128};
+  CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
+  CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
+
+  // whole batches: the shares of all CTAs cover every (sequence, head, query tile, key tile) once, in order; the
+  // CTAs that an item's ends belong to are the ones that walk over them; sequences out of range get nothing
+  for (int round = 0; round < 1500; ++round) {
+    const int n = pick(1, 9), page_shift = pick(4, 7), max_blocks = pick(1, 40), max_q = pick(1, 90);
+    const int most = max_blocks << page_shift;
+    std::vector<int> q_start(n + 1, 0), kv(n), table(n * max_blocks, 0);
+    for (int i = 0; i < n; ++i) {
+      q_start[i + 1] = q_start[i] + (pick(0, 4) ? pick(0, max_q) : 0);
+      kv[i] = pick(0, most);
+      if (pick(0, 30) == 0) kv[i] = pick(0, 1) ? most + 1 : -1;
+    }
+    if (pick(0, 15) == 0) q_start[pick(0, n)] = pick(0, 1) ? -3 : 100000;
+    int status = 0;
+    PagedBatch b{n, pick(0, 5) ? q_start[n] : q_start[n] + 3, max_q, max_blocks, page_shift, 1, q_start.data(), kv.data(),
+                 table.data(), &status};
+    const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2]};
+    std::vector<long long> units(n), begin(n + 1, 0);
+    for (int i = 0; i < n; ++i) {
+      const long long len = static_cast<long long>(q_start[i + 1]) - q_start[i];
+      const bool ok = q_start[i] >= 0 && len >= 0 && q_start[i + 1] <= b.n_tokens && len <= max_q && kv[i] >= 0 && kv[i] <= most;
+      units[i] = seq_units(b, ts, i);
+      CHECK(ok || units[i] == 0);
+      CHECK(!ok || len == 0 || units[i] > 0);
+      if (!ok) CHECK(status == kDevBadLengths);
+      begin[i + 1] = begin[i] + units[i];
+    }
+    const long long total = begin[n];
+    if (!total) continue;
+    const int grid = pick(1, 60), n_cta = share_ctas(total, grid, pick(1, 4));
+    CHECK(n_cta >= 1 && n_cta <= grid);
+    long long u = 0;
+    int seq = -1, head = 0, qt = 0, tile = 0;
+    for (int c = 0; c < n_cta; ++c) {
+      PlanStart s{total, share_begin(total, n_cta, c), share_begin(total, n_cta, c + 1), 0, 0, n_cta};
+      CHECK(s.u0 == u && s.u1 > s.u0);
+      while (begin[s.seq + 1] <= s.u0) ++s.seq;
+      s.seq_begin = begin[s.seq];
+      PieceWalk w;
+      for (bool more = w.begin(b, ts, s); more; more = w.next(b, ts)) {
+        const Piece& p = w.p;
+        CHECK(p.t0 < p.t1 && p.t1 <= p.n_tiles && p.item + p.t0 == u);
+        if (p.t0 == 0) {                    // a new item: the next in order
+          CHECK(tile == 0);
+          if (p.seq != seq) { CHECK(p.seq > seq && p.head == 0 && p.qt == 0); seq = p.seq; head = qt = 0; }
+          CHECK(p.head == head && p.qt == qt);
+        } else {
+          CHECK(p.t0 == tile && p.seq == seq && p.head == head && p.qt == qt);
+        }
+        CHECK(share_of(total, n_cta, p.item + p.t0) == c && share_of(total, n_cta, p.item + p.t1 - 1) == c);
+        u += p.t1 - p.t0;
+        tile = p.t1 == p.n_tiles ? 0 : p.t1;
+        if (tile == 0) {
+          HeadTiles h{p.span.n, p.span.kv, ts.tq, ts.tk};
+          if (++qt == h.n_qt()) { qt = 0; ++head; }
+        }
+      }
+      CHECK(u == s.u1);
+    }
+    CHECK(u == total);
+  }
+  // pages out of range
+  int table[4] = {0, 5, -1, 2}, kv = 64, q0[2] = {0, 1}, status = 0;
+  PagedBatch b{1, 1, 1, 4, 4, 5, q0, &kv, table, &status};
+  CHECK(page_of(b, 0, 15) == 0 && page_of(b, 0, 63) == 2 && status == 0);
+  CHECK(page_of(b, 0, 16) == 5 && status == kDevBadPage);
+  status = 0;
+  CHECK(page_of(b, 0, 32) == 5 && status == kDevBadPage);
+  std::printf("%d\n", bad);
+  return bad != 0;
+}
+"""
+
+
+def test_shares_cover_every_unit_once(tmp_path):
+    src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    src.write_text("#include <algorithm>\n" + BODY)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-I", CSRC,
+                           "-I", os.path.join(CUDA, "include"), "-x", "c++", str(src), "-o", str(exe)])
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-2000:]
