@@ -26,6 +26,8 @@ struct ilre_paged {
   float* part_o;                        // partial results of cut items
   float2* part_ml;
   uint32_t* arrived;
+  float* chunk_o;
+  float2* chunk_ml;
   int32_t* n_keep;                      // rows that an eviction keeps of each sequence
   int* status;
   int last_launches;
@@ -40,7 +42,8 @@ constexpr double kPi = 3.14159265358979323846;
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 void free_all(ilre_paged* h) {
-  cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->status);
+  cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->chunk_o);
+  cudaFree(h->chunk_ml); cudaFree(h->status);
 }
 
 // Full turns per position of every channel pair.
@@ -99,7 +102,7 @@ int validate_batch(const ilre_paged* h, const ilre_paged_batch_t* b, const ilre_
     return ILRE_ERR_CAPACITY;
   int shift = 0;
   while ((1 << shift) < h->cfg.page_size) ++shift;
-  *out = PagedBatch{b->n_seqs, b->n_tokens, b->max_q_len, b->max_blocks, shift, pool->n_pages, b->q_start_dev,
+  *out = PagedBatch{b->n_seqs, b->n_tokens, b->max_q_len, b->max_blocks, shift, pool->n_pages, 0, 2147483647, b->q_start_dev,
                     b->kv_len_dev, b->block_table_dev, h->status};
   return ILRE_OK;
 }
@@ -130,6 +133,18 @@ bool encode_pool(const ilre_paged* h, CUtensorMap* map, const void* base, int64_
   const cuuint32_t estride[4] = {1, 1, 1, 1};
   const CUtensorMapDataType t = h->cfg.dtype == ILRE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   return h->encode(map, t, 4, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Query rows as {channel, head, token}, boxes of 64 channels of one group's heads by 128 / group tokens.
+bool encode_rows(const ilre_paged* h, CUtensorMap* map, const void* base, int64_t stride, int n_tokens, int group) {
+  const cuuint64_t gdim[3] = {kDim, static_cast<cuuint64_t>(h->cfg.n_q_heads), static_cast<cuuint64_t>(n_tokens)};
+  const cuuint64_t gstride[2] = {kDim * 2, static_cast<cuuint64_t>(stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(128 / group)};
+  const cuuint32_t estride[3] = {1, 1, 1};
+  const CUtensorMapDataType t = h->cfg.dtype == ILRE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return h->encode(map, t, 3, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -201,6 +216,8 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
   bool ok = dev_alloc(h, &h->part_o, ctas * 2 * kRowTile * kDim);
   ok = ok && dev_alloc(h, &h->part_ml, ctas * 2 * kRowTile);
   ok = ok && dev_alloc(h, &h->arrived, ctas);
+  ok = ok && dev_alloc(h, &h->chunk_o, static_cast<size_t>(h->n_sm) * 2 * kChunkRows * kDim);
+  ok = ok && dev_alloc(h, &h->chunk_ml, static_cast<size_t>(h->n_sm) * 2 * kChunkRows);
   ok = ok && dev_alloc(h, &h->n_keep, cfg->max_seqs);
   ok = ok && dev_alloc(h, &h->status, 1);
   if (ok) ok = cudaMemset(h->status, 0, sizeof(int)) == cudaSuccess;
@@ -273,13 +290,34 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
   p.part_o = h->part_o; p.part_ml = h->part_ml; p.arrived = h->arrived;
-  CUtensorMap map_k, map_v;
-  const int box = h->cfg.page_size < kRowKeys ? h->cfg.page_size : kRowKeys;
-  if (!encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, box) ||
-      !encode_pool(h, &map_v, pool->v_dev, vs, pool->n_pages, box))
-    return ILRE_ERR_CUDA;
-  ILRE_CUDA(launch_paged_rows(map_k, map_v, p, h->cfg.dtype == ILRE_F16, h->n_sm, st));
-  h->last_launches = 1;
+  p.chunk_o = h->chunk_o; p.chunk_ml = h->chunk_ml;
+  // Sequences whose rows (new tokens x heads of a group) fit one tile of the row kernel are bound by the
+  // reading of the cache and are its; the others' rows share a key tile in the chunk kernel.  The launches
+  // follow from what the host knows: one sequence has one kind, and max_q_len may rule out the second.
+  const bool f16 = h->cfg.dtype == ILRE_F16;
+  const int row_tokens = kRowTile / p.group;             // 0: a group of more than 16 heads
+  const bool chunks = batch->max_q_len > row_tokens;
+  const bool rows = row_tokens > 0 && (!chunks || batch->n_seqs > 1);
+  h->last_launches = 0;
+  CUtensorMap map_q, map_k, map_v;
+  auto maps = [&](int tile_rows) {
+    const int box = h->cfg.page_size < tile_rows ? h->cfg.page_size : tile_rows;
+    return encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, box) &&
+           encode_pool(h, &map_v, pool->v_dev, vs, pool->n_pages, box);
+  };
+  if (rows) {
+    if (!maps(kRowKeys)) return ILRE_ERR_CUDA;
+    if (chunks) p.batch.q_to = row_tokens;
+    ILRE_CUDA(launch_paged_rows(map_k, map_v, p, f16, h->n_sm, st));
+    ++h->last_launches;
+  }
+  if (chunks) {
+    if (!maps(128) || !encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group)) return ILRE_ERR_CUDA;
+    p.batch.q_from = rows ? row_tokens + 1 : 0;
+    p.batch.q_to = 2147483647;
+    ILRE_CUDA(launch_paged_chunk(map_q, map_k, map_v, p, f16, h->n_sm, st));
+    h->last_launches += 2;
+  }
   return ILRE_OK;
 }
 

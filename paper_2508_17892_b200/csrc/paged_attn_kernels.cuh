@@ -12,6 +12,7 @@ namespace ilre {
 static constexpr int kRowTile = 16;              // query rows of a work item of the row kernel
 static constexpr int kRowKeys = 64;              // keys of a stage
 static constexpr int kRowCtasPerSm = 2;
+static constexpr int kChunkRows = 256;           // query rows of a work item of the chunk kernel
 
 struct PagedAttnParams {
   PagedBatch batch;
@@ -24,10 +25,17 @@ struct PagedAttnParams {
   float* part_o;                                 // [CTA][2][rows][128]
   float2* part_ml;                               // [CTA][2][rows]: (maximum in log2 units, sum)
   uint32_t* arrived;                             // [CTA], 0 between launches
+  float* chunk_o;                                // the chunk kernel's: [CTA][2][32][kChunkRows][4]
+  float2* chunk_ml;                              // [CTA][2][kChunkRows]
 };
 
 // map_k, map_v: the pools as {channel, kv head, row, page}, boxes of 64 channels x min(page_size, kRowKeys) rows.
 cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v, const PagedAttnParams& p, bool f16,
                               int n_sm, cudaStream_t st);
+
+// map_q: {channel, head, token}, boxes of 64 channels x group x 128 / group; map_k, map_v: as above with boxes of
+// min(page_size, 128) rows.
+cudaError_t launch_paged_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                               const PagedAttnParams& p, bool f16, int n_sm, cudaStream_t st);
 
 }  // namespace ilre

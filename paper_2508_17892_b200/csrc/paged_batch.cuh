@@ -77,6 +77,7 @@ struct PagedBatch {
   int n_seqs, n_tokens, max_q_len, max_blocks;
   int page_shift;                          // log2(page_size)
   int n_pages;
+  int q_from, q_to;                        // sequences of fewer or more new tokens are another kernel's
   const int32_t* q_start;
   const int32_t* kv_len;
   const int32_t* table;
@@ -104,6 +105,8 @@ __host__ __device__ __forceinline__ SeqSpan load_span(const PagedBatch& b, int i
   return ok ? SeqSpan{a, e - a, kv} : SeqSpan{0, 0, 0};
 }
 
+__host__ __device__ __forceinline__ bool in_range(const PagedBatch& b, int n) { return n >= b.q_from && n <= b.q_to; }
+
 // Page of row t, n_pages (past the pool's end: a TMA load reads zeros there) if the table's entry is none.
 __host__ __device__ __forceinline__ int page_of(const PagedBatch& b, int seq, int t) {
   const int page = b.table[static_cast<long long>(seq) * b.max_blocks + (t >> b.page_shift)];
@@ -119,6 +122,7 @@ struct TileShape {
 
 __host__ __device__ __forceinline__ long long seq_units(const PagedBatch& b, const TileShape& ts, int i) {
   const SeqSpan s = load_span(b, i);
+  if (!in_range(b, s.n)) return 0;
   return HeadTiles{s.n, s.kv, ts.tq, ts.tk}.units() * ts.heads;
 }
 
@@ -177,7 +181,7 @@ struct PieceWalk {
         do {                               // units are left, so a sequence with work follows
           if (++p.seq >= b.n_seqs) return false;
           p.span = load_span(b, p.seq);
-        } while (p.span.n == 0);
+        } while (p.span.n == 0 || !in_range(b, p.span.n));
         tiles = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk};
         n_qt = tiles.n_qt();
       }

@@ -58,7 +58,7 @@ int main() {
     }
     if (pick(0, 15) == 0) q_start[pick(0, n)] = pick(0, 1) ? -3 : 100000;
     int status = 0;
-    PagedBatch b{n, pick(0, 5) ? q_start[n] : q_start[n] + 3, max_q, max_blocks, page_shift, 1, q_start.data(), kv.data(),
+    PagedBatch b{n, pick(0, 5) ? q_start[n] : q_start[n] + 3, max_q, max_blocks, page_shift, 1, 0, 1 << 30, q_start.data(), kv.data(),
                  table.data(), &status};
     const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2]};
     std::vector<long long> units(n), begin(n + 1, 0);
@@ -107,7 +107,7 @@ int main() {
   }
   // pages out of range
   int table[4] = {0, 5, -1, 2}, kv = 64, q0[2] = {0, 1}, status = 0;
-  PagedBatch b{1, 1, 1, 4, 4, 5, q0, &kv, table, &status};
+  PagedBatch b{1, 1, 1, 4, 4, 5, 0, 1 << 30, q0, &kv, table, &status};
   CHECK(page_of(b, 0, 15) == 0 && page_of(b, 0, 63) == 2 && status == 0);
   CHECK(page_of(b, 0, 16) == 5 && status == kDevBadPage);
   status = 0;
