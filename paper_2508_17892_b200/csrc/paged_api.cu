@@ -28,6 +28,7 @@ struct ilre_paged {
   uint32_t* arrived;
   float* chunk_o;
   float2* chunk_ml;
+  ChunkJoin* join;
   int32_t* n_keep;                      // rows that an eviction keeps of each sequence
   int* status;
   int last_launches;
@@ -43,7 +44,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 void free_all(ilre_paged* h) {
   cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->chunk_o);
-  cudaFree(h->chunk_ml); cudaFree(h->status);
+  cudaFree(h->chunk_ml); cudaFree(h->join); cudaFree(h->status);
 }
 
 // Full turns per position of every channel pair.
@@ -218,6 +219,7 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
   ok = ok && dev_alloc(h, &h->arrived, ctas);
   ok = ok && dev_alloc(h, &h->chunk_o, static_cast<size_t>(h->n_sm) * 2 * kChunkRows * kDim);
   ok = ok && dev_alloc(h, &h->chunk_ml, static_cast<size_t>(h->n_sm) * 2 * kChunkRows);
+  ok = ok && dev_alloc(h, &h->join, h->n_sm);
   ok = ok && dev_alloc(h, &h->n_keep, cfg->max_seqs);
   ok = ok && dev_alloc(h, &h->status, 1);
   if (ok) ok = cudaMemset(h->status, 0, sizeof(int)) == cudaSuccess;
@@ -290,7 +292,7 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
   p.part_o = h->part_o; p.part_ml = h->part_ml; p.arrived = h->arrived;
-  p.chunk_o = h->chunk_o; p.chunk_ml = h->chunk_ml;
+  p.chunk_o = h->chunk_o; p.chunk_ml = h->chunk_ml; p.join = h->join;
   // Sequences whose rows (new tokens x heads of a group) fit one tile of the row kernel are bound by the
   // reading of the cache and are its; the others' rows share a key tile in the chunk kernel.  The launches
   // follow from what the host knows: one sequence has one kind, and max_q_len may rule out the second.

@@ -14,6 +14,11 @@ static constexpr int kRowKeys = 64;              // keys of a stage
 static constexpr int kRowCtasPerSm = 2;
 static constexpr int kChunkRows = 256;           // query rows of a work item of the chunk kernel
 
+// The cut item that begins in a CTA's share: its last CTA (-1: there is none), first token, tokens, kv head.
+struct ChunkJoin {
+  int c_last, token, n_tok, head;
+};
+
 struct PagedAttnParams {
   PagedBatch batch;
   const void* q;
@@ -27,6 +32,7 @@ struct PagedAttnParams {
   uint32_t* arrived;                             // [CTA], 0 between launches
   float* chunk_o;                                // the chunk kernel's: [CTA][2][32][kChunkRows][4]
   float2* chunk_ml;                              // [CTA][2][kChunkRows]
+  ChunkJoin* join;                               // [CTA]
 };
 
 // map_k, map_v: the pools as {channel, kv head, row, page}, boxes of 64 channels x min(page_size, kRowKeys) rows.

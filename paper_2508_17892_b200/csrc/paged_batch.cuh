@@ -11,46 +11,46 @@
 
 namespace ilre {
 
-// Sum of floor((a i + b) / m) for i = 0 .. n-1 (a, b >= 0, m >= 1): Euclid's algorithm on the lattice points
-// below the line.
-__host__ __device__ inline long long floor_sum(long long n, long long m, long long a, long long b) {
-  long long ans = 0;
-  while (true) {
-    if (a >= m) { ans += n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) { ans += n * (b / m); b %= m; }
-    const long long y = a * n + b;
-    if (y < m) return ans;
-    n = y / m;
-    b = y % m;
-    const long long t = m; m = a; a = t;
-  }
-}
-
 // One head of one sequence: n query tokens in tiles of `tq`, the last of them seeing all kv rows, keys in tiles
-// of `tk`.  Every query tile has at least one key tile (a tile that sees nothing still writes its output).
+// of 2^tk_shift.  Every query tile has at least one key tile (a tile that sees nothing still writes its output).
+// Lengths stay below 2^31 - 2048, so what a tile sees fits 32 bits; sums take 64.
 struct HeadTiles {
-  int n, kv, tq, tk;
-  __host__ __device__ int n_qt() const { return (n + tq - 1) / tq; }
+  int n, kv, tq, tk_shift;
+  __host__ __device__ int n_qt() const { return static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   __host__ __device__ int key_tiles(int qt) const {
     const long long last = static_cast<long long>(qt + 1) * tq;
-    const long long seen = static_cast<long long>(kv) - n + (last < n ? last : n);
-    return seen <= 0 ? 1 : static_cast<int>((seen + tk - 1) / tk);
+    const int seen = kv - n + (last < n ? static_cast<int>(last) : n);
+    return seen <= 0 ? 1 : static_cast<int>((static_cast<unsigned>(seen) + (1u << tk_shift) - 1) >> tk_shift);
   }
-  // key tiles of the query tiles before qt, qt <= n_qt() - 1
+  // Key tiles of the query tiles before qt <= n_qt() - 1.  Tile i behind those that see nothing counts
+  // f(i) = (b + i tq) >> tk_shift, and f(i + P) = f(i) + s with P a power of two (2 for tq = 64 and 128 keys): k whole
+  // periods and a rest, no division.
   __host__ __device__ long long before(int qt) const {
-    const long long pre = static_cast<long long>(kv) - n;
-    long long blind = pre < 0 ? -pre / tq : 0;            // tiles that see nothing
-    if (blind > qt) blind = qt;
-    return blind + floor_sum(qt - blind, tk, tq, pre + (blind + 1) * tq + tk - 1);
+    const int pre = kv - n;
+    int blind = pre < 0 ? static_cast<int>(static_cast<unsigned>(-pre) / tq) : 0;        // tiles that see nothing
+    if (blind >= qt) return qt;
+    const unsigned b = static_cast<unsigned>(pre + (blind + 1) * tq) + (1u << tk_shift) - 1;
+    int z = 0;
+    while (z < tk_shift && !((tq >> z) & 1)) ++z;
+    const int p_shift = tk_shift - z, P = 1 << p_shift, terms = qt - blind;
+    const long long k = terms >> p_shift, s = tq >> z;
+    const int r = terms & (P - 1);
+    long long whole = 0, rest = 0;
+    for (int i = 0; i < (k ? P : r); ++i) {
+      const unsigned f = (b + static_cast<unsigned>(i) * tq) >> tk_shift;
+      whole += f;
+      if (i < r) rest += f;
+    }
+    return blind + k * whole + s * P * (k * (k - 1) / 2) + rest + s * k * r;
   }
   __host__ __device__ long long units() const {
     if (n <= 0) return 0;
     const int last = n_qt() - 1;
     return before(last) + key_tiles(last);
   }
-  // the query tile that unit u of this head belongs to
+  // the query tile that unit u of this head belongs to: the largest qt with before(qt) <= u
   __host__ __device__ int tile_of(long long u) const {
-    int lo = 0, hi = n_qt() - 1;                           // largest qt with before(qt) <= u
+    int lo = 0, hi = n_qt() - 1;
     while (lo < hi) {
       const int mid = lo + (hi - lo + 1) / 2;
       if (before(mid) <= u) lo = mid; else hi = mid - 1;
@@ -59,14 +59,20 @@ struct HeadTiles {
   }
 };
 
+// x / d of positive numbers; a 64-bit division only where it needs one (it takes some hundred cycles).
+__host__ __device__ inline long long div_pos(long long x, long long d) {
+  if (((x | d) >> 32) == 0) return static_cast<unsigned>(x) / static_cast<unsigned>(d);
+  return x / d;
+}
+
 // Shares: CTA b of n has the units [total b / n, total (b + 1) / n).
-__host__ __device__ inline long long share_begin(long long total, int n, int b) { return total * b / n; }
+__host__ __device__ inline long long share_begin(long long total, int n, int b) { return div_pos(total * b, n); }
 __host__ __device__ inline int share_of(long long total, int n, long long u) {
-  return static_cast<int>(((u + 1) * n - 1) / total);
+  return static_cast<int>(div_pos((u + 1) * n - 1, total));
 }
 // CTAs that get a share: all, or fewer so that none has less than min_units.
 __host__ __device__ inline int share_ctas(long long total, int grid, int min_units) {
-  const long long n = total / min_units;
+  const long long n = div_pos(total, min_units);
   return n < 1 ? 1 : n < grid ? static_cast<int>(n) : grid;
 }
 
@@ -107,34 +113,80 @@ __host__ __device__ __forceinline__ SeqSpan load_span(const PagedBatch& b, int i
 
 __host__ __device__ __forceinline__ bool in_range(const PagedBatch& b, int n) { return n >= b.q_from && n <= b.q_to; }
 
-// Page of row t, n_pages (past the pool's end: a TMA load reads zeros there) if the table's entry is none.
-__host__ __device__ __forceinline__ int page_of(const PagedBatch& b, int seq, int t) {
-  const int page = b.table[static_cast<long long>(seq) * b.max_blocks + (t >> b.page_shift)];
-  if (page >= 0 && page < b.n_pages) return page;
+// Page of row t, n_pages (past the pool's end: a TMA load reads zeros there) if the table's entry is none.  In two
+// steps for loops that ask for an entry well before they need it (the check waits for the load).
+__host__ __device__ __forceinline__ int table_entry(const PagedBatch& b, int seq, int t) {
+  return b.table[static_cast<long long>(seq) * b.max_blocks + (t >> b.page_shift)];
+}
+__host__ __device__ __forceinline__ int checked_page(const PagedBatch& b, int entry) {
+  if (entry >= 0 && entry < b.n_pages) return entry;
   report(b.status, kDevBadPage);
   return b.n_pages;
+}
+__host__ __device__ __forceinline__ int page_of(const PagedBatch& b, int seq, int t) {
+  return checked_page(b, table_entry(b, seq, t));
 }
 
 // Tiles of the batch's heads: `heads` work columns per sequence (kv heads, or parts of their groups).
 struct TileShape {
-  int heads, tq, tk;
+  int heads, tq, tk_shift;
 };
 
 __host__ __device__ __forceinline__ long long seq_units(const PagedBatch& b, const TileShape& ts, int i) {
   const SeqSpan s = load_span(b, i);
   if (!in_range(b, s.n)) return 0;
-  return HeadTiles{s.n, s.kv, ts.tq, ts.tk}.units() * ts.heads;
+  return HeadTiles{s.n, s.kv, ts.tq, ts.tk_shift}.units() * ts.heads;
+}
+
+// The query tile of one head that a unit lies in.
+struct Item {
+  SeqSpan span;
+  int seq, head, qt, n_tiles;              // n_tiles: key tiles
+  long long begin;                         // its first unit
+};
+
+// The query tile of a head's unit.  On the device all lanes of a warp ask together and try 32 tiles at a time.
+__host__ __device__ __forceinline__ int find_tile(const HeadTiles& t, long long u) {
+#ifdef __CUDA_ARCH__
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = t.n_qt();                // in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) >> 5, qt = lo + lane * step;
+    const bool at_or_behind = lane * step < n && t.before(qt) <= u;
+    const int k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, at_or_behind));              // lane 0's is true
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  return lo;
+#else
+  return t.tile_of(u);
+#endif
+}
+
+// The item of unit `at` of the sequence `seq` whose first unit is seq_begin.
+__host__ __device__ __forceinline__ Item locate(const PagedBatch& b, const TileShape& ts, int seq, long long seq_begin,
+                                                long long at) {
+  Item x;
+  x.seq = seq;
+  x.span = load_span(b, seq);
+  const HeadTiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift};
+  const long long per_head = tiles.units(), off = at - seq_begin;
+  x.head = static_cast<int>(div_pos(off, per_head));
+  const long long in_head = off - x.head * per_head;
+  x.qt = find_tile(tiles, in_head);
+  x.begin = at - in_head + tiles.before(x.qt);
+  x.n_tiles = tiles.key_tiles(x.qt);
+  return x;
 }
 
 struct PlanStart {
   long long total;                         // units of the batch
   long long u0, u1;                        // this CTA's share (empty: u0 == u1)
-  long long seq_begin;                     // first unit of sequence `seq`
-  int seq;                                 // the sequence that u0 lies in
+  Item first, last;                        // the items of u0 and u1 - 1
   int n_cta;                               // CTAs that have a share
 };
 
-// A run of key tiles [t0, t1) of one query tile of one head: what a CTA works on at a time.
+// A run of key tiles [t0, t1) of one item: what a CTA works on at a time.
 struct Piece {
   SeqSpan span;
   int seq, head, qt;
@@ -142,37 +194,43 @@ struct Piece {
   long long item;                          // the item's first unit
 };
 
-// The pieces of a CTA's share, one after another.
+// The pieces of a CTA's share: the last one first, then the others in order.  The last piece begins at its item's
+// first keys and the first one usually goes on where another CTA's stops, so that in this order the CTAs that work
+// on query tiles of one sequence pass over its keys side by side, and one of them brings each key tile into L2 for
+// all (1024 tokens behind 31744 rows: ORDER_US).
 struct PieceWalk {
-  long long u, end;
-  HeadTiles tiles;
+  long long u, end;                        // units that follow the current piece
+  bool last;                               // the current piece is the share's last one
   int n_qt;
   Piece p;
 
   // Positions on the first piece; false if the share is empty.
-  __host__ __device__ __forceinline__ bool begin(const PagedBatch& b, const TileShape& ts, const PlanStart& s) {
-    u = s.u0; end = s.u1;
-    if (u >= end) return false;
-    p.seq = s.seq;
-    p.span = load_span(b, p.seq);
-    tiles = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk};
-    n_qt = tiles.n_qt();
-    const long long per_head = tiles.units(), off = u - s.seq_begin;
-    p.head = static_cast<int>(off / per_head);
-    const long long in_head = off - p.head * per_head;
-    p.qt = n_qt == 1 ? 0 : tiles.tile_of(in_head);
-    p.t0 = static_cast<int>(in_head - tiles.before(p.qt));
-    p.item = u - p.t0;
-    p.n_tiles = tiles.key_tiles(p.qt);
-    close();
+  __host__ __device__ __forceinline__ bool begin(const TileShape& ts, const PlanStart& s) {
+    if (s.u0 >= s.u1) return false;
+    last = true;
+    end = s.u1;
+    open(ts, s.last, s.last.begin < s.u0 ? static_cast<int>(s.u0 - s.last.begin) : 0);
     return true;
+  }
+  __host__ __device__ __forceinline__ void open(const TileShape& ts, const Item& x, int t0) {
+    p.span = x.span; p.seq = x.seq; p.head = x.head; p.qt = x.qt; p.n_tiles = x.n_tiles; p.item = x.begin;
+    p.t0 = t0;
+    n_qt = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
+    close();
   }
   __host__ __device__ __forceinline__ void close() {
     const long long left = end - p.item;
     p.t1 = left < p.n_tiles ? static_cast<int>(left) : p.n_tiles;
     u = p.item + p.t1;
   }
-  __host__ __device__ __forceinline__ bool next(const PagedBatch& b, const TileShape& ts) {
+  __host__ __device__ __forceinline__ bool next(const PagedBatch& b, const TileShape& ts, const PlanStart& s) {
+    if (last) {
+      last = false;
+      end = s.last.begin;
+      if (s.u0 >= end) return false;
+      open(ts, s.first, static_cast<int>(s.u0 - s.first.begin));
+      return true;
+    }
     if (u >= end) return false;
     if (++p.qt == n_qt) {
       p.qt = 0;
@@ -182,13 +240,12 @@ struct PieceWalk {
           if (++p.seq >= b.n_seqs) return false;
           p.span = load_span(b, p.seq);
         } while (p.span.n == 0 || !in_range(b, p.span.n));
-        tiles = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk};
-        n_qt = tiles.n_qt();
+        n_qt = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
       }
     }
     p.t0 = 0;
     p.item = u;
-    p.n_tiles = tiles.key_tiles(p.qt);
+    p.n_tiles = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.key_tiles(p.qt);
     close();
     return true;
   }

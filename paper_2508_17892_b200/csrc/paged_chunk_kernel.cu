@@ -137,6 +137,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   }
   plan_start(b, ts, kMinUnits, reinterpret_cast<long long*>(p_ptr), &tail->plan);
   __syncthreads();
+  if (threadIdx.x == 0) {                                // the item that begins here and goes on in other shares
+    const PlanStart& s = tail->plan;
+    ChunkJoin j = {-1, 0, 0, 0};
+    if (s.u0 < s.u1 && s.last.begin >= s.u0 && s.last.begin + s.last.n_tiles > s.u1) {
+      j.c_last = share_of(s.total, s.n_cta, s.last.begin + s.last.n_tiles - 1);
+      j.token = s.last.span.q0 + s.last.qt * ts.tq;
+      j.n_tok = min(ts.tq, s.last.span.n - s.last.qt * ts.tq);
+      j.head = s.last.head;
+    }
+    p.join[blockIdx.x] = j;
+  }
   const bool run = *abort_flag == 0;
   auto streams = [&](const Piece& pc) { return pc.span.n - pc.qt * ts.tq > tok ? 2 : 1; };
 
@@ -153,7 +164,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const bool active = bx < n_box;
     const uint32_t off = half * kHalf + bx * box_rows * 128;
     PieceWalk w;
-    bool ok = run && w.begin(b, ts, tail->plan), more = ok;
+    bool ok = run && w.begin(ts, tail->plan), more = ok;
     int it = 0, n_piece = 0;
     while (more && ok) {
       const Piece& pc = w.p;
@@ -162,10 +173,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         *is_k = i == 0 || ((i & 1) && i != 2 * n - 1);
         return pc.t0 + (i == 0 ? 0 : i == 2 * n - 1 ? n - 1 : *is_k ? (i + 1) / 2 : i / 2 - 1);
       };
-      auto page_at = [&](int t) -> int {                 // rows at and behind kv: zeros, not read
-        const int row = t * 128 + bx * box_rows;
-        return active && row < pc.span.kv ? page_of(b, pc.seq, row) : b.n_pages;
-      };
+      // Table entries: of the key tile to come and of the value tile behind it (the one before), the former asked for a
+      // tile ahead.  Rows at and behind kv need none: zeros, not read.
+      auto needs = [&](int t) { return active && t < pc.t1 && t * 128 + bx * box_rows < pc.span.kv; };
+      auto entry_at = [&](int t) -> int { return needs(t) ? table_entry(b, pc.seq, t * 128 + bx * box_rows) : 0; };
+      int e_k = entry_at(pc.t0), e_v = e_k, e_next = entry_at(pc.t0 + 1);
       ok = warp_wait(&tail->q_empty, (n_piece & 1) ^ 1, abort_flag, b.status, kDevWaitQFull);
       if (!ok) break;
       if (lane == 0) {
@@ -178,16 +190,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       }
       ++n_piece;
       if (lane == 0) tail->q_issued = n_piece;
-      bool is_k;
-      int page = page_at(pc.t0);
       for (int i = 0; i < 2 * n; ++i, ++it) {
+        bool is_k;
         const int t = tile_of_item(i, &is_k);
-        const bool k_now = is_k;
-        const int row = t * 128 + bx * box_rows, cur = page;
-        if (i + 1 < 2 * n) page = page_at(tile_of_item(i + 1, &is_k));
-        const int s = it % kStages;
+        const int row = t * 128 + bx * box_rows, s = it % kStages;
         ok = warp_wait(&tail->kv_empty[s], ((it / kStages) & 1) ^ 1, abort_flag, b.status, kDevWaitKEmpty);
         if (!ok) break;
+        const int page = needs(t) ? checked_page(b, is_k ? e_k : e_v) : b.n_pages;
         const uint32_t bar = smem_u32(&tail->kv_full[s]);
         if (lane == 0) {
           mbar_arrive_expect_tx(bar, kTileBytes);
@@ -195,9 +204,15 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         __syncwarp();
         if (active)
-          tma_load_4d(ring_s + s * kTileBytes + off, k_now ? &map_k : &map_v, half * 64, pc.head, row & (ps - 1), cur, bar);
+          tma_load_4d(ring_s + s * kTileBytes + off, is_k ? &map_k : &map_v, half * 64, pc.head, row & (ps - 1), page, bar);
+        // order K_0, K_1, V_0, K_2, V_1, ...: V_t comes behind K_{t+1}, whose entry then is the next V's
+        if (i == 0 || !is_k) {
+          if (i > 0) e_v = e_k;
+          e_k = e_next;
+          e_next = entry_at(t + (i == 0 ? 2 : 3));
+        }
       }
-      if (ok) more = w.next(b, ts);
+      if (ok) more = w.next(b, ts, tail->plan);
     }
   } else if (warp == 1 || warp == 2) {
     // Two MMA-issuing threads, one for every S = Q K^T, one for every O += P V; each polls its streams' barriers and
@@ -210,7 +225,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       const bool s_role = (warp == 1);
       volatile int* v_landed = &tail->v_landed;
       PieceWalk w;
-      bool ok = w.begin(b, ts, tail->plan), more = ok;
+      bool ok = w.begin(ts, tail->plan), more = ok;
       int it0 = 0, tile0 = 0, n_prev = 2, n_piece = 0;
       uint32_t done[2] = {0, 0};                         // tiles of each stream so far
       int landed = 0;
@@ -301,7 +316,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         tile0 += n;
         n_prev = n;
         ++n_piece;
-        more = w.next(b, ts);
+        more = w.next(b, ts, tail->plan);
       }
     }
   } else {
@@ -320,7 +335,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     uint32_t items = 0;                                  // ring items before this piece
     bool ok = run;
     bool more;
-    if (lane == 0) more = walk->begin(b, ts, tail->plan);
+    if (lane == 0) more = walk->begin(ts, tail->plan);
     more = __shfl_sync(0xFFFFFFFFu, more, 0);
     __syncwarp();
     while (more && ok) {
@@ -498,7 +513,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       if (!ok) break;
       items += 2 * n;
       __syncwarp();
-      if (lane == 0) more = walk->next(b, ts);
+      if (lane == 0) more = walk->next(b, ts, tail->plan);
       more = __shfl_sync(0xFFFFFFFFu, more, 0);
       __syncwarp();
     }
@@ -522,53 +537,55 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // Joins the pieces of the item that begins in share blockIdx.x and goes on behind it, if there is one: thread = query
 // row, blockIdx.y = kJoinChannels of the 128 channels.
 constexpr int kJoinChannels = 16;
+constexpr int kJoinFlight = 4;                           // contributors whose loads are in flight
 
 template <bool kF16>
 __global__ void __launch_bounds__(kChunkRows)
-paged_join_kernel(const __grid_constant__ PagedAttnParams p, const TileShape ts, int grid) {
-  __shared__ long long tmp[34];
-  __shared__ PlanStart plan;
+paged_join_kernel(const __grid_constant__ PagedAttnParams p, int tok) {
   grid_dep_wait();
   grid_dep_launch();
-  const PagedBatch& b = p.batch;
-  plan_last(b, ts, grid, kMinUnits, tmp, &plan);
-  __syncthreads();
-  PieceWalk w;
-  if (!w.begin(b, ts, plan)) return;
-  const int c0 = blockIdx.x;
-  const Piece& pc = w.p;
-  if (pc.item < share_begin(plan.total, plan.n_cta, c0) || pc.item + pc.n_tiles <= share_begin(plan.total, plan.n_cta, c0 + 1))
-    return;
-  const int c1 = share_of(plan.total, plan.n_cta, pc.item + pc.n_tiles - 1);
-  const int tok = ts.tq / 2, row = threadIdx.x, x = row >> 7;
+  const ChunkJoin j = p.join[blockIdx.x];
+  const int c0 = blockIdx.x, c1 = j.c_last;
+  if (c1 < 0) return;
+  const int row = threadIdx.x, x = row >> 7;
   const int rt = (row & 127) / p.group, rh = (row & 127) - rt * p.group;
-  const int my_tok = pc.qt * ts.tq + x * tok + rt;
-  if (rt >= tok || my_tok >= pc.span.n) return;
-  float M = -INFINITY;
+  const int my_tok = x * tok + rt;
+  if (rt >= tok || my_tok >= j.n_tok) return;
+  // kJoinFlight contributors' loads in flight; contributor c0's slot is 1 (the item begins in its share), the others' 0
+  float M = -INFINITY, L = 0.f;
+#pragma unroll 8
   for (int c = c0; c <= c1; ++c) M = fmaxf(M, p.chunk_ml[(c * 2 + (c == c0)) * kChunkRows + row].x);
   const float z = M == -INFINITY ? 0.f : M;
-  float L = 0.f;
   float4 acc[kJoinChannels / 4];
 #pragma unroll
   for (int i = 0; i < kJoinChannels / 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = c0; c <= c1; ++c) {
-    const long long slot = c * 2 + (c == c0);
-    const float2 ml = p.chunk_ml[slot * kChunkRows + row];
-    const float f = ex2_approx(ml.x - z);
-    L = fmaf(ml.y, f, L);
-    const float4* po = reinterpret_cast<const float4*>(p.chunk_o) + slot * (kChunkRows * 32) +
-                       blockIdx.y * (kJoinChannels / 4) * kChunkRows + row;
-    if (f != 0.f) {                                      // a piece in which the row saw nothing may hold anything
+  for (int c = c0; c <= c1; c += kJoinFlight) {
+    float2 ml[kJoinFlight];
+    float4 v[kJoinFlight][kJoinChannels / 4];
 #pragma unroll
-      for (int i = 0; i < kJoinChannels / 4; ++i) {
-        const float4 v = po[i * kChunkRows];
-        acc[i].x = fmaf(v.x, f, acc[i].x); acc[i].y = fmaf(v.y, f, acc[i].y);
-        acc[i].z = fmaf(v.z, f, acc[i].z); acc[i].w = fmaf(v.w, f, acc[i].w);
+    for (int f = 0; f < kJoinFlight; ++f) {
+      const long long slot = min(c + f, c1) * 2 + (c + f == c0);
+      ml[f] = p.chunk_ml[slot * kChunkRows + row];
+      const float4* po = reinterpret_cast<const float4*>(p.chunk_o) + slot * (kChunkRows * 32) +
+                         blockIdx.y * (kJoinChannels / 4) * kChunkRows + row;
+#pragma unroll
+      for (int i = 0; i < kJoinChannels / 4; ++i) v[f][i] = po[i * kChunkRows];
+    }
+#pragma unroll
+    for (int f = 0; f < kJoinFlight; ++f) {
+      const float s = ex2_approx(ml[f].x - z);
+      if (c + f <= c1 && (s != 0.f || isnan(ml[f].y))) {         // where the row saw nothing, O may hold anything
+        L = fmaf(ml[f].y, s, L);
+#pragma unroll
+        for (int i = 0; i < kJoinChannels / 4; ++i) {
+          acc[i].x = fmaf(v[f][i].x, s, acc[i].x); acc[i].y = fmaf(v[f][i].y, s, acc[i].y);
+          acc[i].z = fmaf(v[f][i].z, s, acc[i].z); acc[i].w = fmaf(v[f][i].w, s, acc[i].w);
+        }
       }
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const long long at = (static_cast<long long>(pc.span.q0) + my_tok) * p.n_q + pc.head * p.group + rh;
+  const long long at = (static_cast<long long>(j.token) + my_tok) * p.n_q + j.head * p.group + rh;
   uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * 128 + blockIdx.y * kJoinChannels);
 #pragma unroll
   for (int i = 0; i < kJoinChannels / 4; i += 2)
@@ -585,11 +602,11 @@ cudaError_t launch_paged_chunk(const CUtensorMap& map_q, const CUtensorMap& map_
   auto k = f16 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
   cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
   if (e != cudaSuccess) return e;
-  const TileShape ts = {p.n_kv, 2 * (128 / p.group), 128};
+  const TileShape ts = {p.n_kv, 2 * (128 / p.group), 7};
   e = launch_after_previous(k, n_sm, kThreads, kSmem, st, map_q, map_k, map_v, p, ts);
   if (e != cudaSuccess) return e;
   auto j = f16 ? paged_join_kernel<true> : paged_join_kernel<false>;
-  return launch_after_previous(j, dim3(n_sm, 128 / kJoinChannels), kChunkRows, 0, st, p, ts, n_sm);
+  return launch_after_previous(j, dim3(n_sm, 128 / kJoinChannels), kChunkRows, 0, st, p, 128 / p.group);
 }
 
 }  // namespace ilre

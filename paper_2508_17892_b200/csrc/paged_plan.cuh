@@ -4,7 +4,9 @@
 
 namespace ilre {
 
-// Units of the whole batch: all threads of the CTA; `tmp` holds 34 entries in shared memory.  *mine: the units of
+static constexpr int kPlanTmp = 36;
+
+// Units of the whole batch: all threads of the CTA; `tmp` holds kPlanTmp entries in shared memory.  *mine: the units of
 // the sequences that this thread looked at (its own one, if the batch has no more than the CTA threads).
 __device__ __forceinline__ long long plan_total(const PagedBatch& b, const TileShape& ts, long long* tmp, long long* mine) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (blockDim.x + 31) >> 5;
@@ -20,10 +22,11 @@ __device__ __forceinline__ long long plan_total(const PagedBatch& b, const TileS
   return total;
 }
 
-// The sequence that unit u0 lies in, and its first unit, into *out (valid behind a barrier).
+// The items of units u0 and u1 - 1 into *out (valid behind a barrier).
 __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& ts, long long mine, long long u0,
-                                          long long* tmp, PlanStart* out) {
+                                          long long u1, long long* tmp, PlanStart* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (blockDim.x + 31) >> 5;
+  long long* found = tmp + 32;             // (sequence, first unit) of u0 and of u1 - 1
   long long base = 0;
   for (int i0 = 0; i0 < b.n_seqs; i0 += blockDim.x) {
     const int i = i0 + threadIdx.x;
@@ -41,39 +44,27 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
       base += tmp[w];
     }
     const long long begin = before + incl - n;
-    if (n > 0 && begin <= u0 && u0 < begin + n) { out->seq = i; out->seq_begin = begin; }
+    if (n > 0 && begin <= u0 && u0 < begin + n) { found[0] = i; found[1] = begin; }
+    if (n > 0 && begin < u1 && u1 <= begin + n) { found[2] = i; found[3] = begin; }
     __syncthreads();
-    if (base > u0) break;
+    if (base >= u1) break;
+  }
+  if (warp < 2) {
+    const Item x = locate(b, ts, static_cast<int>(found[2 * warp]), found[2 * warp + 1], warp ? u1 - 1 : u0);
+    if (lane == 0) { if (warp) out->last = x; else out->first = x; }
   }
 }
 
-// The units [u0, u1) as a share of its own: all threads; *out is valid behind the next barrier.
-__device__ __forceinline__ void plan_range(const PagedBatch& b, const TileShape& ts, long long total, int n_cta,
-                                           long long mine, long long u0, long long u1, long long* tmp, PlanStart* out) {
-  if (threadIdx.x == 0) { out->total = total; out->n_cta = n_cta; out->u0 = u0; out->u1 = u1; out->seq = 0; out->seq_begin = 0; }
-  __syncthreads();
-  if (u0 < u1) plan_find(b, ts, mine, u0, tmp, out);
-}
-
-// This CTA's share.
+// This CTA's share: all threads; *out is valid behind the next barrier.
 __device__ __forceinline__ void plan_start(const PagedBatch& b, const TileShape& ts, int min_units, long long* tmp,
                                            PlanStart* out) {
   long long mine;
   const long long total = plan_total(b, ts, tmp, &mine);
   const int n_cta = share_ctas(total, gridDim.x, min_units), c = blockIdx.x;
   const bool has = total > 0 && c < n_cta;
-  plan_range(b, ts, total, n_cta, mine, has ? share_begin(total, n_cta, c) : 0, has ? share_begin(total, n_cta, c + 1) : 0, tmp, out);
-}
-
-// The last unit of the share that CTA blockIdx.x of `grid` had; nothing for the last share of all.
-__device__ __forceinline__ void plan_last(const PagedBatch& b, const TileShape& ts, int grid, int min_units, long long* tmp,
-                                          PlanStart* out) {
-  long long mine;
-  const long long total = plan_total(b, ts, tmp, &mine);
-  const int n_cta = share_ctas(total, grid, min_units), c = blockIdx.x;
-  const bool has = total > 0 && c + 1 < n_cta;
-  const long long end = has ? share_begin(total, n_cta, c + 1) : 0;
-  plan_range(b, ts, total, n_cta, mine, has ? end - 1 : 0, end, tmp, out);
+  const long long u0 = has ? share_begin(total, n_cta, c) : 0, u1 = has ? share_begin(total, n_cta, c + 1) : 0;
+  if (threadIdx.x == 0) { out->total = total; out->n_cta = n_cta; out->u0 = u0; out->u1 = u1; }
+  if (has) plan_find(b, ts, mine, u0, u1, tmp, out);
 }
 
 }  // namespace ilre

@@ -27,13 +27,14 @@ constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kWarps = 4;                                // consumers
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kMergeFloats = kRowTile * 128;             // output of one warp on its way to another
+constexpr int kJoinFlight = 8;                           // partial results in flight
 constexpr int kMinUnits = 2;                             // 64-key tiles that a CTA gets at least
 
 struct RowTail {
   uint64_t full[kStages];
   uint64_t empty[kStages];
   PlanStart plan;
-  long long tmp[34];
+  long long tmp[kPlanTmp];
   float2 ml[kWarps][kRowTile];
   int abort_flag;
   int last;
@@ -103,9 +104,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
   plan_start(b, ts, kMinUnits, tail->tmp, &tail->plan);
   __syncthreads();
-  const PlanStart plan = tail->plan;
+  const PlanStart& plan = tail->plan;
   PieceWalk w;
-  if (!w.begin(b, ts, plan)) return;
+  if (!w.begin(ts, plan)) return;
   bool ok = *abort_flag == 0;
 
   if (warp == kWarps) {
@@ -117,27 +118,28 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const uint32_t off = is_v * kTileBytes + half * kHalfBytes + bx * box_rows * 128;
     int it = 0;
     bool more = true;
-    auto page_at = [&](int t) -> int {                   // rows at and behind kv: zeros, not read
-      const int row = t * kRowKeys + bx * box_rows;
-      return active && row < w.p.span.kv ? page_of(b, w.p.seq, row) : b.n_pages;
-    };
+    // Entries two tiles ahead; rows at and behind kv need none: zeros, not read.
+    auto needs = [&](int t) { return active && t < w.p.t1 && t * kRowKeys + bx * box_rows < w.p.span.kv; };
+    auto entry_at = [&](int t) -> int { return needs(t) ? table_entry(b, w.p.seq, t * kRowKeys + bx * box_rows) : 0; };
     while (more && ok) {
       const int g = w.p.head / rs.parts;
-      int page = page_at(w.p.t0);
+      int e0 = entry_at(w.p.t0), e1 = entry_at(w.p.t0 + 1);
       for (int t = w.p.t0; t < w.p.t1; ++t, ++it) {
         const int s = it % kStages;
-        const int row = t * kRowKeys + bx * box_rows, cur = page;
-        if (t + 1 < w.p.t1) page = page_at(t + 1);
+        const int row = t * kRowKeys + bx * box_rows, e2 = entry_at(t + 2);
         ok = mbar_wait(smem_u32(&tail->empty[s]), ((it / kStages) & 1) ^ 1, abort_flag, b.status, kDevWaitKEmpty);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
+        const int page = needs(t) ? checked_page(b, e0) : b.n_pages;
         const uint32_t bar = smem_u32(&tail->full[s]);
         if (lane == 0) mbar_arrive_expect_tx(bar, kStageBytes);
         __syncwarp();
         if (active)
-          tma_load_4d(ring + s * kStageBytes + off, is_v ? &map_v : &map_k, half * 64, g, row & (ps - 1), cur, bar);
+          tma_load_4d(ring + s * kStageBytes + off, is_v ? &map_v : &map_k, half * 64, g, row & (ps - 1), page, bar);
+        e0 = e1;
+        e1 = e2;
       }
-      if (ok) more = w.next(b, ts);
+      if (ok) more = w.next(b, ts, tail->plan);
     }
     return;
   }
@@ -325,31 +327,52 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
       sync_consumers();
       if (tail->last && ok) {
-        // thread = channel; contributor c's slot is 1 if the item begins in it, else 0
-        const int ch = threadIdx.x;
-        for (int r = 0; r < kRowTile; ++r) {
+        // A row per warp: the contributors' factors by the lanes into shared memory, then four channels per lane.
+        // Contributor c's slot is 1 if the item begins in it, else 0.
+        const int n = b_last - b_first + 1;
+        float* factor = merge + warp * (kMergeFloats / 2);                     // n <= 2 CTAs x SMs
+        for (int r = warp; r < kRowTile; r += kWarps) {
           if (!row_valid(r)) continue;
           float M = -INFINITY;
-          for (int c = b_first; c <= b_last; ++c) M = fmaxf(M, __ldcg(&p.part_ml[(c * 2 + (c == b_first)) * kRowTile + r]).x);
+          for (int c = lane; c < n; c += 32) M = fmaxf(M, __ldcg(&p.part_ml[((b_first + c) * 2 + (c == 0)) * kRowTile + r]).x);
+          for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
           const float z = M == -INFINITY ? 0.f : M;
-          float L = 0.f, acc = 0.f;
-          for (int c = b_first; c <= b_last; ++c) {
-            const int sl = c * 2 + (c == b_first);
-            const float2 ml = __ldcg(&p.part_ml[sl * kRowTile + r]);
+          float L = 0.f;
+          for (int c = lane; c < n; c += 32) {
+            const float2 ml = __ldcg(&p.part_ml[((b_first + c) * 2 + (c == 0)) * kRowTile + r]);
             const float f = ex2_approx(ml.x - z);
+            factor[c] = f;
             L = fmaf(ml.y, f, L);
-            acc = fmaf(__ldcg(p.part_o + static_cast<long long>(sl) * kMergeFloats + r * 128 + ch), f, acc);
           }
-          const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+          for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+          __syncwarp();
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c0 = 0; c0 < n; c0 += kJoinFlight) {
+            float4 v[kJoinFlight];
+#pragma unroll
+            for (int i = 0; i < kJoinFlight; ++i) {
+              const int c = min(c0 + i, n - 1);
+              v[i] = __ldcg(reinterpret_cast<const float4*>(
+                  p.part_o + static_cast<long long>((b_first + c) * 2 + (c == 0)) * kMergeFloats + r * 128) + lane);
+            }
+#pragma unroll
+            for (int i = 0; i < kJoinFlight; ++i) {
+              const float f = c0 + i < n ? factor[c0 + i] : 0.f;
+              acc.x = fmaf(v[i].x, f, acc.x); acc.y = fmaf(v[i].y, f, acc.y);
+              acc.z = fmaf(v[i].z, f, acc.z); acc.w = fmaf(v[i].w, f, acc.w);
+            }
+          }
+          __syncwarp();
+          const float inv = L == 0.f ? 0.f : 1.f / L;
           const long long at = row_elem(r) * p.n_q + h_first + r % rs.hs;
-          if (kF16) static_cast<__half*>(p.out)[at * 128 + ch] = __float2half_rn(acc * inv);
-          else static_cast<__nv_bfloat16*>(p.out)[at * 128 + ch] = __float2bfloat16_rn(acc * inv);
-          if (p.lse && ch == 0) p.lse[at] = (M + log2f(L)) * 0.69314718f;
+          uint2* dst = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * 128) + lane;
+          *dst = make_uint2(pack2<kF16>(acc.x * inv, acc.y * inv), pack2<kF16>(acc.z * inv, acc.w * inv));
+          if (p.lse && lane == 0) p.lse[at] = (M + log2f(L)) * 0.69314718f;
         }
       }
       sync_consumers();                                  // tail->last is written again by the next piece
     }
-  } while (w.next(b, ts));
+  } while (w.next(b, ts, tail->plan));
 }
 
 constexpr size_t kSmem = kStages * kStageBytes + 2 * kMergeFloats * 4 + sizeof(RowTail);
@@ -365,7 +388,7 @@ cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v
   RowShape rs;
   rs.hs = p.group < kRowTile ? p.group : kRowTile;
   rs.parts = (p.group + rs.hs - 1) / rs.hs;
-  const TileShape ts = {p.n_kv * rs.parts, kRowTile / rs.hs, kRowKeys};
+  const TileShape ts = {p.n_kv * rs.parts, kRowTile / rs.hs, 6};
   return launch_after_previous(k, n_sm * kRowCtasPerSm, kThreads, kSmem, st, map_k, map_v, p, ts, rs);
 }
 

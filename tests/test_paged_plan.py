@@ -20,20 +20,14 @@ static int bad = 0;
 int main() {
   std::mt19937 rng(7);
   auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
-  for (int i = 0; i < 20000; ++i) {
-    const long long n = pick(0, 40), m = pick(1, 130), a = pick(0, 300), b = pick(0, 3000);
-    long long want = 0;
-    for (long long j = 0; j < n; ++j) want += (a * j + b) / m;
-    CHECK(floor_sum(n, m, a, b) == want);
-  }
   // one head: units, their prefix sums and the tile of each unit
-  const int tqs[] = {1, 2, 4, 16, 36, 64, 256}, tks[] = {64, 128};
+  const int tqs[] = {1, 2, 4, 16, 50, 64, 256}, tks[] = {6, 7};
   for (int i = 0; i < 4000; ++i) {
     HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2]};
     long long at = 0;
     for (int qt = 0; qt < h.n_qt(); ++qt) {
       const int last = std::min((qt + 1) * h.tq, h.n), seen = h.kv - h.n + last;
-      CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + h.tk - 1) / h.tk));
+      CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + (1 << h.tk_shift) - 1) >> h.tk_shift));
       CHECK(h.before(qt) == at);
       for (long long u = at; u < at + h.key_tiles(qt); u += 3) CHECK(h.tile_of(u) == qt);
       at += h.key_tiles(qt);
@@ -41,7 +35,7 @@ int main() {
     CHECK(h.units() == at);
   }
   // far lengths: no overflow
-  HeadTiles far{1 << 30, 2147481000, 64, 128};
+  HeadTiles far{1 << 30, 2147481000, 64, 7};
   CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
   CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
 
@@ -78,13 +72,21 @@ int main() {
     long long u = 0;
     int seq = -1, head = 0, qt = 0, tile = 0;
     for (int c = 0; c < n_cta; ++c) {
-      PlanStart s{total, share_begin(total, n_cta, c), share_begin(total, n_cta, c + 1), 0, 0, n_cta};
+      PlanStart s;
+      s.total = total; s.n_cta = n_cta;
+      s.u0 = share_begin(total, n_cta, c); s.u1 = share_begin(total, n_cta, c + 1);
       CHECK(s.u0 == u && s.u1 > s.u0);
-      while (begin[s.seq + 1] <= s.u0) ++s.seq;
-      s.seq_begin = begin[s.seq];
+      int a = 0, z = 0;
+      while (begin[a + 1] <= s.u0) ++a;
+      while (begin[z + 1] < s.u1) ++z;
+      s.first = locate(b, ts, a, begin[a], s.u0);
+      s.last = locate(b, ts, z, begin[z], s.u1 - 1);
       PieceWalk w;
-      for (bool more = w.begin(b, ts, s); more; more = w.next(b, ts)) {
-        const Piece& p = w.p;
+      std::vector<Piece> pieces;            // the last one comes first
+      for (bool more = w.begin(ts, s); more; more = w.next(b, ts, s)) pieces.push_back(w.p);
+      CHECK(pieces[0].item + pieces[0].t1 == s.u1);
+      std::rotate(pieces.begin(), pieces.begin() + 1, pieces.end());
+      for (const Piece& p : pieces) {
         CHECK(p.t0 < p.t1 && p.t1 <= p.n_tiles && p.item + p.t0 == u);
         if (p.t0 == 0) {                    // a new item: the next in order
           CHECK(tile == 0);
@@ -97,7 +99,7 @@ int main() {
         u += p.t1 - p.t0;
         tile = p.t1 == p.n_tiles ? 0 : p.t1;
         if (tile == 0) {
-          HeadTiles h{p.span.n, p.span.kv, ts.tq, ts.tk};
+          HeadTiles h{p.span.n, p.span.kv, ts.tq, ts.tk_shift};
           if (++qt == h.n_qt()) { qt = 0; ++head; }
         }
       }
