@@ -29,6 +29,7 @@ struct ilre_paged {
   float* chunk_o;
   float2* chunk_ml;
   ChunkJoin* join;
+  float* w_part;
   int32_t* n_keep;                      // rows that an eviction keeps of each sequence
   int* status;
   int last_launches;
@@ -44,7 +45,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 void free_all(ilre_paged* h) {
   cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->chunk_o);
-  cudaFree(h->chunk_ml); cudaFree(h->join); cudaFree(h->status);
+  cudaFree(h->chunk_ml); cudaFree(h->join); cudaFree(h->w_part); cudaFree(h->status);
 }
 
 // Full turns per position of every channel pair.
@@ -138,11 +139,12 @@ bool encode_pool(const ilre_paged* h, CUtensorMap* map, const void* base, int64_
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Query rows as {channel, head, token}, boxes of 64 channels of one group's heads by 128 / group tokens.
-bool encode_rows(const ilre_paged* h, CUtensorMap* map, const void* base, int64_t stride, int n_tokens, int group) {
+// Query rows as {channel, head, token}, boxes of 64 channels of one group's heads by box_tokens tokens.
+bool encode_rows(const ilre_paged* h, CUtensorMap* map, const void* base, int64_t stride, int n_tokens, int group,
+                 int box_tokens) {
   const cuuint64_t gdim[3] = {kDim, static_cast<cuuint64_t>(h->cfg.n_q_heads), static_cast<cuuint64_t>(n_tokens)};
   const cuuint64_t gstride[2] = {kDim * 2, static_cast<cuuint64_t>(stride) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(128 / group)};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(box_tokens)};
   const cuuint32_t estride[3] = {1, 1, 1};
   const CUtensorMapDataType t = h->cfg.dtype == ILRE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   return h->encode(map, t, 3, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -220,6 +222,7 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
   ok = ok && dev_alloc(h, &h->chunk_o, static_cast<size_t>(h->n_sm) * 2 * kChunkRows * kDim);
   ok = ok && dev_alloc(h, &h->chunk_ml, static_cast<size_t>(h->n_sm) * 2 * kChunkRows);
   ok = ok && dev_alloc(h, &h->join, h->n_sm);
+  ok = ok && dev_alloc(h, &h->w_part, static_cast<size_t>(h->n_sm) * 2 * 128);
   ok = ok && dev_alloc(h, &h->n_keep, cfg->max_seqs);
   ok = ok && dev_alloc(h, &h->status, 1);
   if (ok) ok = cudaMemset(h->status, 0, sizeof(int)) == cudaSuccess;
@@ -314,7 +317,8 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
     ++h->last_launches;
   }
   if (chunks) {
-    if (!maps(128) || !encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group)) return ILRE_ERR_CUDA;
+    if (!maps(128) || !encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group, 128 / p.group))
+      return ILRE_ERR_CUDA;
     p.batch.q_from = rows ? row_tokens + 1 : 0;
     p.batch.q_to = 2147483647;
     ILRE_CUDA(launch_paged_chunk(map_q, map_k, map_v, p, f16, h->n_sm, st));
@@ -338,11 +342,15 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   h->last_stream = st;
-  p.q = q_dev; p.q_stride = q_stride; p.k = pool->k_dev; p.k_page_stride = ks;
   p.lse = lse_dev; p.w = pool->w_dev;
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
-  ILRE_CUDA(launch_paged_weights(p, h->cfg.dtype == ILRE_F16, st));
+  p.part = h->w_part; p.arrived = h->arrived;
+  CUtensorMap map_q, map_k;
+  if (!encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group, weight_tile_tokens(p.group, batch->max_q_len)) ||
+      !encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, h->cfg.page_size < 128 ? h->cfg.page_size : 128))
+    return ILRE_ERR_CUDA;
+  ILRE_CUDA(launch_paged_weights(map_q, map_k, p, h->cfg.dtype == ILRE_F16, h->n_sm, st));
   h->last_launches = 1;
   return ILRE_OK;
 }

@@ -59,6 +59,55 @@ struct HeadTiles {
   }
 };
 
+// The same split seen from the keys, for sums over the query rows: an item is a tile of 2^tk_shift keys, its units are
+// the tiles of `tq` query tokens that see any of them.  (The names are HeadTiles': "query tile" is the item's
+// number, "key tiles" are its units.)
+struct KeyTiles {
+  int n, kv, tq, tk_shift;
+  __host__ __device__ int n_qt() const { return static_cast<int>((static_cast<unsigned>(kv) + (1u << tk_shift) - 1) >> tk_shift); }
+  __host__ __device__ int row_tiles() const { return static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
+  // the first row tile that sees a key of tile kt
+  __host__ __device__ int first(int kt) const {
+    const int tok = (kt << tk_shift) - (kv - n);
+    return tok <= 0 ? 0 : static_cast<int>(static_cast<unsigned>(tok) / tq);
+  }
+  __host__ __device__ int key_tiles(int kt) const { return row_tiles() - first(kt); }
+  // Units of the key tiles before kt: all row tiles less those that see none, first(i) = (b + i 2^tk_shift) / tq from
+  // key tile `seen` on, which repeats with a period of tq / gcd.
+  __host__ __device__ long long before(int kt) const {
+    const int pre = kv - n;
+    const int seen = pre <= 0 ? 0 : static_cast<int>((static_cast<unsigned>(pre) + (1u << tk_shift) - 1) >> tk_shift);
+    const long long all = static_cast<long long>(kt) * row_tiles();
+    if (seen >= kt) return all;
+    const unsigned b = static_cast<unsigned>((seen << tk_shift) - pre);
+    int z = 0;
+    while (z < tk_shift && !((tq >> z) & 1)) ++z;
+    const int P = tq >> z, s = 1 << (tk_shift - z), terms = kt - seen;
+    const long long k = terms / P;
+    const int r = terms - static_cast<int>(k) * P;
+    long long whole = 0, rest = 0;
+    for (int i = 0; i < (k ? P : r); ++i) {
+      const unsigned f = (b + (static_cast<unsigned>(i) << tk_shift)) / tq;
+      whole += f;
+      if (i < r) rest += f;
+    }
+    return all - (k * whole + static_cast<long long>(s) * P * (k * (k - 1) / 2) + rest + s * k * r);
+  }
+  __host__ __device__ long long units() const {
+    if (n <= 0 || kv <= 0) return 0;
+    const int last = n_qt() - 1;
+    return before(last) + key_tiles(last);
+  }
+  __host__ __device__ int tile_of(long long u) const {
+    int lo = 0, hi = n_qt() - 1;
+    while (lo < hi) {
+      const int mid = lo + (hi - lo + 1) / 2;
+      if (before(mid) <= u) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  }
+};
+
 // x / d of positive numbers; a 64-bit division only where it needs one (it takes some hundred cycles).
 __host__ __device__ inline long long div_pos(long long x, long long d) {
   if (((x | d) >> 32) == 0) return static_cast<unsigned>(x) / static_cast<unsigned>(d);
@@ -132,10 +181,11 @@ struct TileShape {
   int heads, tq, tk_shift;
 };
 
+template <class Tiles>
 __host__ __device__ __forceinline__ long long seq_units(const PagedBatch& b, const TileShape& ts, int i) {
   const SeqSpan s = load_span(b, i);
   if (!in_range(b, s.n)) return 0;
-  return HeadTiles{s.n, s.kv, ts.tq, ts.tk_shift}.units() * ts.heads;
+  return Tiles{s.n, s.kv, ts.tq, ts.tk_shift}.units() * ts.heads;
 }
 
 // The query tile of one head that a unit lies in.
@@ -146,7 +196,8 @@ struct Item {
 };
 
 // The query tile of a head's unit.  On the device all lanes of a warp ask together and try 32 tiles at a time.
-__host__ __device__ __forceinline__ int find_tile(const HeadTiles& t, long long u) {
+template <class Tiles>
+__host__ __device__ __forceinline__ int find_tile(const Tiles& t, long long u) {
 #ifdef __CUDA_ARCH__
   const int lane = threadIdx.x & 31;
   int lo = 0, n = t.n_qt();                // in [lo, lo + n)
@@ -164,12 +215,13 @@ __host__ __device__ __forceinline__ int find_tile(const HeadTiles& t, long long 
 }
 
 // The item of unit `at` of the sequence `seq` whose first unit is seq_begin.
+template <class Tiles>
 __host__ __device__ __forceinline__ Item locate(const PagedBatch& b, const TileShape& ts, int seq, long long seq_begin,
                                                 long long at) {
   Item x;
   x.seq = seq;
   x.span = load_span(b, seq);
-  const HeadTiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift};
+  const Tiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift};
   const long long per_head = tiles.units(), off = at - seq_begin;
   x.head = static_cast<int>(div_pos(off, per_head));
   const long long in_head = off - x.head * per_head;
@@ -198,6 +250,7 @@ struct Piece {
 // first keys and the first one usually goes on where another CTA's stops, so that in this order the CTAs that work
 // on query tiles of one sequence pass over its keys side by side, and one of them brings each key tile into L2 for
 // all (1024 tokens behind 31744 rows: ORDER_US).
+template <class Tiles>
 struct PieceWalk {
   long long u, end;                        // units that follow the current piece
   bool last;                               // the current piece is the share's last one
@@ -215,7 +268,7 @@ struct PieceWalk {
   __host__ __device__ __forceinline__ void open(const TileShape& ts, const Item& x, int t0) {
     p.span = x.span; p.seq = x.seq; p.head = x.head; p.qt = x.qt; p.n_tiles = x.n_tiles; p.item = x.begin;
     p.t0 = t0;
-    n_qt = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
+    n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
     close();
   }
   __host__ __device__ __forceinline__ void close() {
@@ -239,13 +292,13 @@ struct PieceWalk {
         do {                               // units are left, so a sequence with work follows
           if (++p.seq >= b.n_seqs) return false;
           p.span = load_span(b, p.seq);
-        } while (p.span.n == 0 || !in_range(b, p.span.n));
-        n_qt = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
+        } while (!in_range(b, p.span.n) || Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.units() == 0);
+        n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
       }
     }
     p.t0 = 0;
     p.item = u;
-    p.n_tiles = HeadTiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.key_tiles(p.qt);
+    p.n_tiles = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.key_tiles(p.qt);
     close();
     return true;
   }

@@ -39,7 +39,7 @@ struct ChunkTail {
   uint64_t kv_empty[kStages];
   uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2], o_full[2];      // per stream
   PlanStart plan;
-  PieceWalk walk[2 * kSoftmaxWarps];                     // one per softmax warp
+  PieceWalk<HeadTiles> walk[2 * kSoftmaxWarps];                     // one per softmax warp
   uint32_t tmem_base;
   int abort_flag;
   int v_landed;                                          // value tiles that the PV thread has seen arrive
@@ -67,10 +67,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A whole warp's bounded wait: all lanes leave it with the same answer.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
-  return __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), parity, abort_flag, status, code));
-}
 // A whole warp's bounded wait for a count in shared memory.
 __device__ __forceinline__ bool warp_wait_count(volatile int* count, int least, volatile int* abort_flag, int* status, int code) {
   bool ok = true;
@@ -135,7 +131,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     tail->abort_flag = 1;
     report(b.status, kDevSmemAlign);
   }
-  plan_start(b, ts, kMinUnits, reinterpret_cast<long long*>(p_ptr), &tail->plan);
+  plan_start<HeadTiles>(b, ts, kMinUnits, reinterpret_cast<long long*>(p_ptr), &tail->plan);
   __syncthreads();
   if (threadIdx.x == 0) {                                // the item that begins here and goes on in other shares
     const PlanStart& s = tail->plan;
@@ -163,7 +159,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const int half = lane & 1, bx = lane >> 1;
     const bool active = bx < n_box;
     const uint32_t off = half * kHalf + bx * box_rows * 128;
-    PieceWalk w;
+    PieceWalk<HeadTiles> w;
     bool ok = run && w.begin(ts, tail->plan), more = ok;
     int it = 0, n_piece = 0;
     while (more && ok) {
@@ -224,7 +220,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       constexpr uint32_t idesc_o = idesc<kF16>(128, 128) | (1u << 16);     // B = V: channels contiguous
       const bool s_role = (warp == 1);
       volatile int* v_landed = &tail->v_landed;
-      PieceWalk w;
+      PieceWalk<HeadTiles> w;
       bool ok = w.begin(ts, tail->plan), more = ok;
       int it0 = 0, tile0 = 0, n_prev = 2, n_piece = 0;
       uint32_t done[2] = {0, 0};                         // tiles of each stream so far
@@ -330,7 +326,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t s_tm = lane_base + x * 128, o_tm = lane_base + 256 + x * 128;
     uint8_t* p_mine = p_ptr + x * kTileBytes;
     const float c2 = p.c2;
-    PieceWalk* walk = &tail->walk[warp - 3];
+    PieceWalk<HeadTiles>* walk = &tail->walk[warp - 3];
     uint32_t n_tile = 0, n_out = 0;                      // of this stream so far
     uint32_t items = 0;                                  // ring items before this piece
     bool ok = run;

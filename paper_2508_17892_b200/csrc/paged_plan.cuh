@@ -8,10 +8,11 @@ static constexpr int kPlanTmp = 36;
 
 // Units of the whole batch: all threads of the CTA; `tmp` holds kPlanTmp entries in shared memory.  *mine: the units of
 // the sequences that this thread looked at (its own one, if the batch has no more than the CTA threads).
+template <class Tiles>
 __device__ __forceinline__ long long plan_total(const PagedBatch& b, const TileShape& ts, long long* tmp, long long* mine) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (blockDim.x + 31) >> 5;
   long long sum = 0;
-  for (int i = threadIdx.x; i < b.n_seqs; i += blockDim.x) sum += seq_units(b, ts, i);
+  for (int i = threadIdx.x; i < b.n_seqs; i += blockDim.x) sum += seq_units<Tiles>(b, ts, i);
   *mine = sum;
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) tmp[warp] = sum;
@@ -23,6 +24,7 @@ __device__ __forceinline__ long long plan_total(const PagedBatch& b, const TileS
 }
 
 // The items of units u0 and u1 - 1 into *out (valid behind a barrier).
+template <class Tiles>
 __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& ts, long long mine, long long u0,
                                           long long u1, long long* tmp, PlanStart* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (blockDim.x + 31) >> 5;
@@ -30,7 +32,7 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
   long long base = 0;
   for (int i0 = 0; i0 < b.n_seqs; i0 += blockDim.x) {
     const int i = i0 + threadIdx.x;
-    const long long n = (i < b.n_seqs) ? (b.n_seqs <= static_cast<int>(blockDim.x) ? mine : seq_units(b, ts, i)) : 0;
+    const long long n = (i < b.n_seqs) ? (b.n_seqs <= static_cast<int>(blockDim.x) ? mine : seq_units<Tiles>(b, ts, i)) : 0;
     long long incl = n;
     for (int o = 1; o < 32; o <<= 1) {
       const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
@@ -50,21 +52,22 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
     if (base >= u1) break;
   }
   if (warp < 2) {
-    const Item x = locate(b, ts, static_cast<int>(found[2 * warp]), found[2 * warp + 1], warp ? u1 - 1 : u0);
+    const Item x = locate<Tiles>(b, ts, static_cast<int>(found[2 * warp]), found[2 * warp + 1], warp ? u1 - 1 : u0);
     if (lane == 0) { if (warp) out->last = x; else out->first = x; }
   }
 }
 
 // This CTA's share: all threads; *out is valid behind the next barrier.
+template <class Tiles>
 __device__ __forceinline__ void plan_start(const PagedBatch& b, const TileShape& ts, int min_units, long long* tmp,
                                            PlanStart* out) {
   long long mine;
-  const long long total = plan_total(b, ts, tmp, &mine);
+  const long long total = plan_total<Tiles>(b, ts, tmp, &mine);
   const int n_cta = share_ctas(total, gridDim.x, min_units), c = blockIdx.x;
   const bool has = total > 0 && c < n_cta;
   const long long u0 = has ? share_begin(total, n_cta, c) : 0, u1 = has ? share_begin(total, n_cta, c + 1) : 0;
   if (threadIdx.x == 0) { out->total = total; out->n_cta = n_cta; out->u0 = u0; out->u1 = u1; }
-  if (has) plan_find(b, ts, mine, u0, u1, tmp, out);
+  if (has) plan_find<Tiles>(b, ts, mine, u0, u1, tmp, out);
 }
 
 }  // namespace ilre

@@ -102,10 +102,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     tail->abort_flag = 1;
     report(b.status, kDevSmemAlign);
   }
-  plan_start(b, ts, kMinUnits, tail->tmp, &tail->plan);
+  plan_start<HeadTiles>(b, ts, kMinUnits, tail->tmp, &tail->plan);
   __syncthreads();
   const PlanStart& plan = tail->plan;
-  PieceWalk w;
+  PieceWalk<HeadTiles> w;
   if (!w.begin(ts, plan)) return;
   bool ok = *abort_flag == 0;
 

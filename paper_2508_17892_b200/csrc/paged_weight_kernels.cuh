@@ -11,14 +11,12 @@ namespace ilre {
 
 struct PagedWeightParams {
   PagedBatch batch;
-  const void* q;
-  long long q_stride;
-  const void* k;                                 // pool
-  long long k_page_stride;
   const float* lse;                              // [n_tokens][n_q]
   float* w;                                      // [n_pages][n_kv][page_size]
   int n_q, n_kv, group;
   float c2;
+  float* part;                                   // [CTA][2][128]: sums of the pieces of cut items
+  uint32_t* arrived;                             // [CTA], 0 between launches
 };
 
 struct EvictParams {
@@ -35,7 +33,12 @@ struct EvictParams {
   int32_t* n_keep;                               // workspace [max_seqs]: rows that stay, -1: sequence left out
 };
 
-cudaError_t launch_paged_weights(const PagedWeightParams& p, bool f16, cudaStream_t st);
+// Query tokens of a row tile: 128 rows, or all that any sequence has.
+int weight_tile_tokens(int group, int max_q_len);
+// map_q: {channel, head, token}, boxes of 64 channels x group x weight_tile_tokens; map_k: the pool as {channel, kv head,
+// row, page}, boxes of 64 channels x min(page_size, 128) rows.
+cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& map_k, const PagedWeightParams& p, bool f16,
+                                 int n_sm, cudaStream_t st);
 cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st);
 
 }  // namespace ilre

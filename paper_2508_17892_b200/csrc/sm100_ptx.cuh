@@ -83,6 +83,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
 }
 
+// A whole warp's bounded wait: all lanes leave it with the same answer.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), parity, abort_flag, status, code));
+}
 // 2-D tiled TMA load, completion counted in bytes on an mbarrier of this CTA.
 __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap* map, int c0,
                                             int c1, uint32_t bar) {

@@ -17,28 +17,20 @@ using namespace ilre;
 static int bad = 0;
 #define CHECK(c) do { if (!(c) && bad++ < 10) std::printf("line %d: %s\n", __LINE__, #c); } while (0)
 
-int main() {
-  std::mt19937 rng(7);
-  auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
-  // one head: units, their prefix sums and the tile of each unit
-  const int tqs[] = {1, 2, 4, 16, 50, 64, 256}, tks[] = {6, 7};
-  for (int i = 0; i < 4000; ++i) {
-    HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2]};
-    long long at = 0;
-    for (int qt = 0; qt < h.n_qt(); ++qt) {
-      const int last = std::min((qt + 1) * h.tq, h.n), seen = h.kv - h.n + last;
-      CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + (1 << h.tk_shift) - 1) >> h.tk_shift));
-      CHECK(h.before(qt) == at);
-      for (long long u = at; u < at + h.key_tiles(qt); u += 3) CHECK(h.tile_of(u) == qt);
-      at += h.key_tiles(qt);
-    }
-    CHECK(h.units() == at);
-  }
-  // far lengths: no overflow
-  HeadTiles far{1 << 30, 2147481000, 64, 7};
-  CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
-  CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
 
+const int tqs[] = {1, 2, 4, 16, 50, 64, 256}, tks[] = {6, 7};
+struct Q : HeadTiles {
+  Q(int n, int kv, int tq, int tk) : HeadTiles{n, kv, tq, tk} {}
+  static bool counts(int) { return true; }
+};
+struct K : KeyTiles {
+  K(int n, int kv, int tq, int tk) : KeyTiles{n, kv, tq, tk} {}
+  static bool counts(int kv) { return kv > 0; }
+};
+
+template <class Tiles>
+void batches(std::mt19937& rng) {
+  auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
   // whole batches: the shares of all CTAs cover every (sequence, head, query tile, key tile) once, in order; the
   // CTAs that an item's ends belong to are the ones that walk over them; sequences out of range get nothing
   for (int round = 0; round < 1500; ++round) {
@@ -59,9 +51,9 @@ int main() {
     for (int i = 0; i < n; ++i) {
       const long long len = static_cast<long long>(q_start[i + 1]) - q_start[i];
       const bool ok = q_start[i] >= 0 && len >= 0 && q_start[i + 1] <= b.n_tokens && len <= max_q && kv[i] >= 0 && kv[i] <= most;
-      units[i] = seq_units(b, ts, i);
+      units[i] = seq_units<Tiles>(b, ts, i);
       CHECK(ok || units[i] == 0);
-      CHECK(!ok || len == 0 || units[i] > 0);
+      CHECK(!ok || len == 0 || (units[i] > 0) == Tiles::counts(kv[i]));
       if (!ok) CHECK(status == kDevBadLengths);
       begin[i + 1] = begin[i] + units[i];
     }
@@ -79,9 +71,9 @@ int main() {
       int a = 0, z = 0;
       while (begin[a + 1] <= s.u0) ++a;
       while (begin[z + 1] < s.u1) ++z;
-      s.first = locate(b, ts, a, begin[a], s.u0);
-      s.last = locate(b, ts, z, begin[z], s.u1 - 1);
-      PieceWalk w;
+      s.first = locate<Tiles>(b, ts, a, begin[a], s.u0);
+      s.last = locate<Tiles>(b, ts, z, begin[z], s.u1 - 1);
+      PieceWalk<Tiles> w;
       std::vector<Piece> pieces;            // the last one comes first
       for (bool more = w.begin(ts, s); more; more = w.next(b, ts, s)) pieces.push_back(w.p);
       CHECK(pieces[0].item + pieces[0].t1 == s.u1);
@@ -99,7 +91,7 @@ int main() {
         u += p.t1 - p.t0;
         tile = p.t1 == p.n_tiles ? 0 : p.t1;
         if (tile == 0) {
-          HeadTiles h{p.span.n, p.span.kv, ts.tq, ts.tk_shift};
+          Tiles h{p.span.n, p.span.kv, ts.tq, ts.tk_shift};
           if (++qt == h.n_qt()) { qt = 0; ++head; }
         }
       }
@@ -107,6 +99,51 @@ int main() {
     }
     CHECK(u == total);
   }
+}
+
+int main() {
+  std::mt19937 rng(7);
+  auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
+  // one head: units, their prefix sums and the tile of each unit
+  for (int i = 0; i < 4000; ++i) {
+    HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2]};
+    long long at = 0;
+    for (int qt = 0; qt < h.n_qt(); ++qt) {
+      const int last = std::min((qt + 1) * h.tq, h.n), seen = h.kv - h.n + last;
+      CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + (1 << h.tk_shift) - 1) >> h.tk_shift));
+      CHECK(h.before(qt) == at);
+      for (long long u = at; u < at + h.key_tiles(qt); u += 3) CHECK(h.tile_of(u) == qt);
+      at += h.key_tiles(qt);
+    }
+    CHECK(h.units() == at);
+  }
+  // the same from the keys: the row tiles that see a key of the tile
+  const int tts[] = {1, 2, 3, 18, 25, 32, 42, 128};
+  for (int i = 0; i < 4000; ++i) {
+    KeyTiles h{pick(1, 400), pick(1, 3) > 1 ? pick(1, 2000) : pick(1, 5), tts[rng() % 8], 7};
+    long long at = 0;
+    for (int kt = 0; kt < h.n_qt(); ++kt) {
+      int seen = 0;
+      for (int r = 0; r * h.tq < h.n; ++r) {
+        const int last = std::min((r + 1) * h.tq, h.n) - 1;            // its last token sees the most
+        if (h.kv - h.n + last >= kt * 128) ++seen;
+      }
+      CHECK(seen >= 1 && h.key_tiles(kt) == seen && h.first(kt) == h.row_tiles() - seen);
+      CHECK(h.before(kt) == at);
+      for (long long u = at; u < at + seen; u += 3) CHECK(h.tile_of(u) == kt);
+      at += seen;
+    }
+    CHECK(h.units() == at);
+  }
+  // far lengths: no overflow
+  HeadTiles far{1 << 30, 2147481000, 64, 7};
+  CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
+  CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
+  KeyTiles far_k{1 << 30, 2147481000, 18, 7};
+  CHECK(far_k.tile_of(far_k.units() - 1) == far_k.n_qt() - 1 && far_k.key_tiles(far_k.n_qt() - 1) >= 1);
+
+  batches<Q>(rng);
+  batches<K>(rng);
   // pages out of range
   int table[4] = {0, 5, -1, 2}, kv = 64, q0[2] = {0, 1}, status = 0;
   PagedBatch b{1, 1, 1, 4, 4, 5, 0, 1 << 30, q0, &kv, table, &status};
