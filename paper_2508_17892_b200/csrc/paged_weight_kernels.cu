@@ -8,8 +8,8 @@
 //
 // What bounds it: with few rows (decoding) the reading of the keys, 256 bytes for 256 flop per row; with many the
 // exponentials, one per logit, of which a quarter are polynomials on the FMA pipe.  One warp loads (a key tile per
-// item, a row tile per unit), one thread issues the MMAs into four accumulators, eight warps in two groups take turns
-// with the accumulators.
+// item, a row tile per unit), one thread issues the MMAs into four accumulators, sixteen warps in four groups have an
+// accumulator each.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -23,29 +23,28 @@ namespace {
 
 constexpr int kKeySlots = 4, kRowSlots = 3, kAccs = 4;
 constexpr int kTileBytes = 128 * 128 * 2, kHalf = kTileBytes / 2;
-constexpr int kThreads = 320;                            // warp 0 loads, 1 MMAs, 2..5 and 6..9 sums
+constexpr int kGroups = 4;                               // of four warps, one per accumulator
+constexpr int kThreads = 64 + kGroups * 128;             // warp 0 loads, 1 MMAs, the others sum
 constexpr int kPolyPairs = 4;                            // of 16 pairs of exponentials, those on the FMA pipe
 
 struct WeightTail {
   uint64_t k_full[kKeySlots], k_empty[kKeySlots], q_full[kRowSlots], q_empty[kRowSlots], d_full[kAccs], d_empty[kAccs];
   PlanStart plan;
-  float lse[2][2][128];                                  // [group][parity][row], log2 units
-  float sums[128];                                       // [key]: the second group's
+  float lse[kGroups][128];                               // [group][row], log2 units; then the group's sums [key]
   uint32_t tmem_base;
   int abort_flag;
   int k_issued, q_issued;
-  int last[2];                                           // [parity]
+  int last[kGroups];
 };
 constexpr size_t kSmem = static_cast<size_t>(kKeySlots + kRowSlots) * kTileBytes + sizeof(WeightTail);
 static_assert(kSmem <= 232448, "shared memory");
 
 __device__ __forceinline__ void sync_group(int group) { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); }
-__device__ __forceinline__ void sync_sums() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void sync_sums() { asm volatile("bar.sync 1, %0;" ::"n"(kGroups * 128) : "memory"); }
 
-// This thread's sum over kCols columns (a multiple of 16, at most 32) of its key: all of them, or those in [lo, hi).
-template <int kCols>
-__device__ __forceinline__ float column_sum(const float (&v)[kCols], const float* lse2, float c2, bool masked, int lo, int hi) {
-  float2 sum = make_float2(0.f, 0.f);
+// This thread's sum over kCols columns (at most 32) of its key: all of them, or those in [lo, hi).
+template <int kCols, bool kMasked>
+__device__ __forceinline__ float2 column_sum(float2 sum, const float (&v)[kCols], const float* lse2, float c2, int lo, int hi) {
 #pragma unroll
   for (int j = 0; j < kCols; j += 4) {
     const float4 n = *reinterpret_cast<const float4*>(lse2 + j);
@@ -54,7 +53,7 @@ __device__ __forceinline__ float column_sum(const float (&v)[kCols], const float
     auto poly = [](int pair) { return ((pair + 1) * kPolyPairs) / 16 > (pair * kPolyPairs) / 16; };
     float2 ea = poly((j >> 1) & 15) ? exp2_poly2(a) : make_float2(ex2_approx(a.x), ex2_approx(a.y));
     float2 eb = poly(((j >> 1) + 1) & 15) ? exp2_poly2(b) : make_float2(ex2_approx(b.x), ex2_approx(b.y));
-    if (masked) {
+    if (kMasked) {
       ea.x = (j >= lo && j < hi) ? ea.x : 0.f;
       ea.y = (j + 1 >= lo && j + 1 < hi) ? ea.y : 0.f;
       eb.x = (j + 2 >= lo && j + 2 < hi) ? eb.x : 0.f;
@@ -62,7 +61,7 @@ __device__ __forceinline__ float column_sum(const float (&v)[kCols], const float
     }
     sum = fadd2(sum, fadd2(ea, eb));
   }
-  return sum.x + sum.y;
+  return sum;
 }
 
 template <bool kF16>
@@ -188,7 +187,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const int gi = threadIdx.x - 64 - group * 128;       // its number in the group
     const int row_tok = gi / p.group, row_head = gi - row_tok * p.group;
     const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
-    int n_row = 0, mine = 0, n_piece = 0;                // units before this piece; of this group; pieces
+    int n_row = 0;                                       // units before this piece
     while (more) {
       const Piece& pc = w.p;
       const int n = pc.t1 - pc.t0, r_first = first_tile(pc), pre = pc.span.kv - pc.span.n;
@@ -202,13 +201,14 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const float v = p.lse[(static_cast<long long>(pc.span.q0) + tok) * p.n_q + pc.head * p.group + row_head];
         return v == -INFINITY ? INFINITY : v * 1.44269504f;
       };
-      int u = (n_row & 1) == group ? 0 : 1;              // units alternate between the groups
+      int u = (group - n_row) & (kGroups - 1);           // unit i is group i % kGroups'
       float lse_next = u < n ? row_lse(pc.t0 + u) : 0.f;
-      float sum = 0.f;
-      for (; u < n && ok; u += 2, ++mine) {
-        float* lse2 = tail->lse[group][mine & 1];
+      float2 sum2 = make_float2(0.f, 0.f);
+      for (; u < n && ok; u += kGroups) {
+        float* lse2 = tail->lse[group];
+        sync_group(group);                               // its last readers are done
         lse2[gi] = lse_next;
-        if (u + 2 < n) lse_next = row_lse(pc.t0 + u + 2);
+        if (u + kGroups < n) lse_next = row_lse(pc.t0 + u + kGroups);
         sync_group(group);
         const int ds = (n_row + u) % kAccs;
         ok = warp_wait(&tail->d_full[ds], ((n_row + u) / kAccs) & 1, abort_flag, b.status, kDevWaitAccFull);
@@ -220,43 +220,45 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int lo = (key - pre - tok0) * p.group;
         const bool masked = hi < tile_rows || pc.qt * 128 + 127 > pre + tok0;
         const uint32_t d = lane_base + ds * 128;
+        // (loops that are not unrolled: the code stays in the instruction cache, the other groups cover the waits)
         if (n_cols == 16) {
           float v[16];
           tmem_ld16(d, v);
           tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&tail->d_empty[ds]));
-          sum += column_sum<16>(v, lse2, p.c2, masked, lo, hi);
+          sum2 = masked ? column_sum<16, true>(sum2, v, lse2, p.c2, lo, hi) : column_sum<16, false>(sum2, v, lse2, p.c2, 0, 0);
+        } else if (masked) {
+#pragma unroll 1
+          for (int c = 0; c < n_cols; c += 32) {
+            float v[32];
+            tmem_ld32(d + c, v);
+            tmem_ld_wait();
+            sum2 = column_sum<32, true>(sum2, v, lse2 + c, p.c2, lo - c, hi - c);
+          }
         } else {
-          float v[2][32];
-          tmem_ld32(d, v[0]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c * 32 >= n_cols) break;
-            const bool again = (c + 1) * 32 < n_cols;
-            if (again) tmem_ld32(d + (c + 1) * 32, v[(c + 1) & 1]);
-            if (!again) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(smem_u32(&tail->d_empty[ds]));
-            }
-            sum += column_sum<32>(v[c & 1], lse2 + c * 32, p.c2, masked, lo - c * 32, hi - c * 32);
-            if (again) tmem_ld_wait();
+#pragma unroll 1
+          for (int c = 0; c < n_cols; c += 32) {
+            float v[32];
+            tmem_ld32(d + c, v);
+            tmem_ld_wait();
+            sum2 = column_sum<32, false>(sum2, v, lse2 + c, p.c2, 0, 0);
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&tail->d_empty[ds]));
       }
-      // ---- one sum per key: the groups' two halves, then to the pool, or to the workspace where the item is cut
+      float sum = sum2.x + sum2.y;
+      // ---- one sum per key: the groups' shares, then to the pool, or to the workspace where the item is cut
       const bool whole = pc.t0 == 0 && pc.t1 == pc.n_tiles;
-      const int par = n_piece & 1;
       int owner = 0;
       if (n == 1) {
-        owner = n_row & 1;
+        owner = n_row & (kGroups - 1);
       } else {
-        if (group == 1) tail->sums[key_lane] = sum;
+        sync_group(group);
+        tail->lse[group][key_lane] = sum;
         sync_sums();
-        if (group == 0) sum += tail->sums[key_lane];
+        if (group == 0)
+          for (int g = 1; g < kGroups; ++g) sum += tail->lse[g][key_lane];
         sync_sums();
       }
       if (group == owner) {
@@ -267,11 +269,11 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           __threadfence();
           sync_group(group);
           if (gi == 0) {                                 // wraps to 0 with the last arrival
-            tail->last[par] = atomicInc(p.arrived + c0, c1 - c0) == static_cast<uint32_t>(c1 - c0);
+            tail->last[group] = atomicInc(p.arrived + c0, c1 - c0) == static_cast<uint32_t>(c1 - c0);
             __threadfence();
           }
           sync_group(group);
-          write = tail->last[par] != 0;
+          write = tail->last[group] != 0;
           if (write) {
             sum = 0.f;
             for (int c = c0; c <= c1; ++c) sum += __ldcg(p.part + (c * 2 + (c == c0)) * 128 + key_lane);
@@ -284,7 +286,6 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
       }
       n_row += n;
-      ++n_piece;
       more = w.next(b, ts, plan);
     }
   }
