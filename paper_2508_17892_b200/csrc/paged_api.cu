@@ -395,6 +395,8 @@ int ilre_paged_status(ilre_paged_t* h) {
   ILRE_CUDA(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));
   if (word == 0) return ILRE_OK;
   ILRE_CUDA(cudaMemset(h->status, 0, sizeof(int)));
+  // a kernel that gave up (now or behind another fault) may not have counted all arrivals
+  ILRE_CUDA(cudaMemset(h->arrived, 0, static_cast<size_t>(h->n_sm) * kRowCtasPerSm * sizeof(uint32_t)));
   return (word == kDevBadLengths || word == kDevBadPage) ? ILRE_ERR_BATCH : ILRE_ERR_DEVICE_WAIT;
 }
 

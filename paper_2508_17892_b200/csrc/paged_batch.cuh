@@ -16,7 +16,7 @@ namespace ilre {
 // Lengths stay below 2^31 - 2048, so what a tile sees fits 32 bits; sums take 64.
 struct HeadTiles {
   int n, kv, tq, tk_shift;
-  __host__ __device__ int n_qt() const { return static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
+  __host__ __device__ int n_qt() const { return n <= tq ? (n > 0) : static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   __host__ __device__ int key_tiles(int qt) const {
     const long long last = static_cast<long long>(qt + 1) * tq;
     const int seen = kv - n + (last < n ? static_cast<int>(last) : n);
@@ -65,11 +65,11 @@ struct HeadTiles {
 struct KeyTiles {
   int n, kv, tq, tk_shift;
   __host__ __device__ int n_qt() const { return static_cast<int>((static_cast<unsigned>(kv) + (1u << tk_shift) - 1) >> tk_shift); }
-  __host__ __device__ int row_tiles() const { return static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
+  __host__ __device__ int row_tiles() const { return n <= tq ? 1 : static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   // the first row tile that sees a key of tile kt
   __host__ __device__ int first(int kt) const {
     const int tok = (kt << tk_shift) - (kv - n);
-    return tok <= 0 ? 0 : static_cast<int>(static_cast<unsigned>(tok) / tq);
+    return tok <= 0 || n <= tq ? 0 : static_cast<int>(static_cast<unsigned>(tok) / tq);
   }
   __host__ __device__ int key_tiles(int kt) const { return row_tiles() - first(kt); }
   // Units of the key tiles before kt: all row tiles less those that see none, first(i) = (b + i 2^tk_shift) / tq from

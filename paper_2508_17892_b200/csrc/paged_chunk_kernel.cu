@@ -67,21 +67,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A whole warp's bounded wait for a count in shared memory.
-__device__ __forceinline__ bool warp_wait_count(volatile int* count, int least, volatile int* abort_flag, int* status, int code) {
-  bool ok = true;
-  const long long t0 = clock64();
-  while (*count < least && ok) {
-    if (*abort_flag) ok = false;
-    if (clock64() - t0 > kWaitCycleLimit) {
-      *abort_flag = 1;
-      atomicCAS(status, 0, code);
-      ok = false;
-    }
-  }
-  return __all_sync(0xFFFFFFFFu, ok);
-}
-
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,

@@ -87,6 +87,21 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
   return __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), parity, abort_flag, status, code));
 }
+// A whole warp's bounded wait for a count in shared memory.
+__device__ __forceinline__ bool warp_wait_count(volatile int* count, int least, volatile int* abort_flag, int* status, int code) {
+  bool ok = true;
+  const long long t0 = clock64();
+  while (*count < least && ok) {
+    if (*abort_flag) ok = false;
+    if (clock64() - t0 > kWaitCycleLimit) {
+      *abort_flag = 1;
+      atomicCAS(status, 0, code);
+      ok = false;
+    }
+  }
+  return __all_sync(0xFFFFFFFFu, ok);
+}
+
 // 2-D tiled TMA load, completion counted in bytes on an mbarrier of this CTA.
 __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap* map, int c0,
                                             int c1, uint32_t bar) {
