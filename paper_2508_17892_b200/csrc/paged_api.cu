@@ -154,6 +154,21 @@ bool encode_rows(const ilre_paged* h, CUtensorMap* map, const void* base, int64_
 
 float softmax_scale() { return static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kDim))); }
 
+// Sequences whose rows (new tokens x heads of a group) fit one tile of 16 are bound by the reading of the cache and
+// go to the row kernels; the others' rows share a key tile in the tensor-core kernels.  The launches follow from what
+// the host knows: one sequence has one kind, and max_q_len may rule out the second.
+struct KernelChoice {
+  int row_tokens;                                        // most new tokens of the first kind; 0: more than 16 heads
+  bool rows, chunks;
+};
+KernelChoice choose_kernels(const ilre_paged_batch_t& b, int group) {
+  KernelChoice c;
+  c.row_tokens = kRowTile / group;
+  c.chunks = b.max_q_len > c.row_tokens;
+  c.rows = c.row_tokens > 0 && (!c.chunks || b.n_seqs > 1);
+  return c;
+}
+
 #define ILRE_CHECK(expr)                \
   do {                                  \
     const int rc_ = (expr);             \
@@ -296,13 +311,8 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
   p.c2 = softmax_scale();
   p.part_o = h->part_o; p.part_ml = h->part_ml; p.arrived = h->arrived;
   p.chunk_o = h->chunk_o; p.chunk_ml = h->chunk_ml; p.join = h->join;
-  // Sequences whose rows (new tokens x heads of a group) fit one tile of the row kernel are bound by the
-  // reading of the cache and are its; the others' rows share a key tile in the chunk kernel.  The launches
-  // follow from what the host knows: one sequence has one kind, and max_q_len may rule out the second.
   const bool f16 = h->cfg.dtype == ILRE_F16;
-  const int row_tokens = kRowTile / p.group;             // 0: a group of more than 16 heads
-  const bool chunks = batch->max_q_len > row_tokens;
-  const bool rows = row_tokens > 0 && (!chunks || batch->n_seqs > 1);
+  const KernelChoice use = choose_kernels(*batch, p.group);
   h->last_launches = 0;
   CUtensorMap map_q, map_k, map_v;
   auto maps = [&](int tile_rows) {
@@ -310,16 +320,16 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
     return encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, box) &&
            encode_pool(h, &map_v, pool->v_dev, vs, pool->n_pages, box);
   };
-  if (rows) {
+  if (use.rows) {
     if (!maps(kRowKeys)) return ILRE_ERR_CUDA;
-    if (chunks) p.batch.q_to = row_tokens;
+    if (use.chunks) p.batch.q_to = use.row_tokens;
     ILRE_CUDA(launch_paged_rows(map_k, map_v, p, f16, h->n_sm, st));
     ++h->last_launches;
   }
-  if (chunks) {
+  if (use.chunks) {
     if (!maps(128) || !encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group, 128 / p.group))
       return ILRE_ERR_CUDA;
-    p.batch.q_from = rows ? row_tokens + 1 : 0;
+    p.batch.q_from = use.rows ? use.row_tokens + 1 : 0;
     p.batch.q_to = 2147483647;
     ILRE_CUDA(launch_paged_chunk(map_q, map_k, map_v, p, f16, h->n_sm, st));
     h->last_launches += 2;
@@ -346,12 +356,26 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
   p.part = h->w_part; p.arrived = h->arrived;
+  p.q = q_dev; p.q_stride = q_stride;
+  const bool f16 = h->cfg.dtype == ILRE_F16;
+  const KernelChoice use = choose_kernels(*batch, p.group);
+  h->last_launches = 0;
   CUtensorMap map_q, map_k;
-  if (!encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group, weight_tile_tokens(p.group, batch->max_q_len)) ||
-      !encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, h->cfg.page_size < 128 ? h->cfg.page_size : 128))
+  if (!encode_pool(h, &map_k, pool->k_dev, ks, pool->n_pages, h->cfg.page_size < 128 ? h->cfg.page_size : 128))
     return ILRE_ERR_CUDA;
-  ILRE_CUDA(launch_paged_weights(map_q, map_k, p, h->cfg.dtype == ILRE_F16, h->n_sm, st));
-  h->last_launches = 1;
+  if (use.rows) {
+    if (use.chunks) p.batch.q_to = use.row_tokens;
+    ILRE_CUDA(launch_paged_weight_rows(map_k, p, f16, h->n_sm, st));
+    ++h->last_launches;
+  }
+  if (use.chunks) {
+    if (!encode_rows(h, &map_q, q_dev, q_stride, batch->n_tokens, p.group, weight_tile_tokens(p.group, batch->max_q_len)))
+      return ILRE_ERR_CUDA;
+    p.batch.q_from = use.rows ? use.row_tokens + 1 : 0;
+    p.batch.q_to = 2147483647;
+    ILRE_CUDA(launch_paged_weights(map_q, map_k, p, f16, h->n_sm, st));
+    ++h->last_launches;
+  }
   return ILRE_OK;
 }
 

@@ -13,11 +13,9 @@
 // tensor memory go on from piece to piece, the next piece's first logits are computed while the last one's output is
 // written.  An item that the cut divides leaves 32-bit partial outputs, which a second kernel joins in the order of the
 // CTAs.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include "launch.cuh"
 #include "paged_attn_kernels.cuh"
+#include "paged_mma.cuh"
 #include "paged_plan.cuh"
 
 namespace ilre {
@@ -57,16 +55,6 @@ template <bool kF16>
 __host__ __device__ constexpr uint32_t idesc(int M, int N) {      // operand types: bits 7 and 10, f16 0, bf16 1
   return kF16 ? umma_idesc_bf16(M, N) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(M, N);
 }
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  if (kF16) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,

@@ -11,6 +11,8 @@ namespace ilre {
 
 struct PagedWeightParams {
   PagedBatch batch;
+  const void* q;                                 // read by the row kernel without a map
+  long long q_stride;
   const float* lse;                              // [n_tokens][n_q]
   float* w;                                      // [n_pages][n_kv][page_size]
   int n_q, n_kv, group;
@@ -39,6 +41,9 @@ int weight_tile_tokens(int group, int max_q_len);
 // row, page}, boxes of 64 channels x min(page_size, 128) rows.
 cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& map_k, const PagedWeightParams& p, bool f16,
                                  int n_sm, cudaStream_t st);
+// Sequences of at most 16 rows (new tokens x heads of a group).
+cudaError_t launch_paged_weight_rows(const CUtensorMap& map_k, const PagedWeightParams& p, bool f16, int n_sm,
+                                     cudaStream_t st);
 cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st);
 
 }  // namespace ilre

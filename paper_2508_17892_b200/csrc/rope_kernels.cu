@@ -10,10 +10,8 @@
 //
 // One thread moves 2 x 16 bytes at a time: the two halves of eight pairs (or 16 channels next to each other), four
 // such items in flight.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include "launch.cuh"
+#include "paged_mma.cuh"
 #include "rope_kernels.cuh"
 
 namespace ilre {
@@ -29,16 +27,6 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
   if (kF16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  if (kF16) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // (cos, sin) of the CTA's tokens: [token][vector 0..3][segment], two pairs per float4, so that the eight threads of a
 // head read 16 bytes each without bank conflicts.
 struct Angles {
