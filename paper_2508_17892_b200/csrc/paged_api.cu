@@ -48,10 +48,18 @@ void free_all(ilre_paged* h) {
   cudaFree(h->chunk_ml); cudaFree(h->join); cudaFree(h->w_part); cudaFree(h->status);
 }
 
-// Full turns per position of every channel pair.
+// Full turns per position of every channel pair.  The last spec's are kept per thread: their powers take longer than a
+// small call's launch.
 int make_freqs(const ilre_rope_spec_t* s, int head_dim, RopeFreqs* f) {
-  std::memset(f, 0, sizeof(*f));
-  if (!s) return ILRE_OK;                                // nothing turns
+  struct Last {
+    ilre_rope_spec_t spec;
+    RopeFreqs freqs;
+  };
+  thread_local Last last;                                // rotary_dim 0 before the first
+  if (!s) {                                              // nothing turns
+    std::memset(f, 0, sizeof(*f));
+    return ILRE_OK;
+  }
   if (!(s->theta > 1.0) || !std::isfinite(s->theta) || s->rotary_dim < 1 || s->layout < ILRE_ROPE_HALF ||
       s->layout > ILRE_ROPE_INTERLEAVED || s->scaling < ILRE_ROPE_PLAIN || s->scaling > ILRE_ROPE_YARN ||
       !(s->attn_factor >= 0.0) || !std::isfinite(s->attn_factor))
@@ -63,6 +71,14 @@ int make_freqs(const ilre_rope_spec_t* s, int head_dim, RopeFreqs* f) {
     return ILRE_ERR_INVALID_ARG;
   if (s->rotary_dim % 16 != 0 || s->rotary_dim > head_dim || s->rotary_dim > 2 * kRopeMaxPairs)
     return ILRE_ERR_UNSUPPORTED;
+  const ilre_rope_spec_t& o = last.spec;
+  if (last.freqs.rotary_dim != 0 && o.theta == s->theta && o.rotary_dim == s->rotary_dim && o.layout == s->layout &&
+      o.scaling == s->scaling && o.factor == s->factor && o.orig_len == s->orig_len && o.low == s->low &&
+      o.high == s->high && o.attn_factor == s->attn_factor) {
+    *f = last.freqs;
+    return ILRE_OK;
+  }
+  std::memset(f, 0, sizeof(*f));
   const int R = s->rotary_dim;
   double lo = 0.0, hi = 0.0;
   if (s->scaling == ILRE_ROPE_YARN) {
@@ -88,6 +104,8 @@ int make_freqs(const ilre_rope_spec_t* s, int head_dim, RopeFreqs* f) {
   f->scale = static_cast<float>(s->attn_factor > 0.0 ? s->attn_factor : own);
   f->rotary_dim = R;
   f->interleaved = s->layout == ILRE_ROPE_INTERLEAVED;
+  last.spec = *s;
+  last.freqs = *f;
   return ILRE_OK;
 }
 
@@ -227,6 +245,11 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
   h->n_sm = prop.multiProcessorCount;
   h->encode = tensor_map_encoder();
   if (!h->encode) {
+    delete h;
+    return ILRE_ERR_CUDA;
+  }
+  if (init_paged_rows() != cudaSuccess || init_paged_chunk() != cudaSuccess || init_paged_weights() != cudaSuccess ||
+      init_paged_weight_rows() != cudaSuccess || init_evict() != cudaSuccess) {
     delete h;
     return ILRE_ERR_CUDA;
   }
@@ -405,7 +428,8 @@ int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t b
   p.n_kv = h->cfg.n_kv_heads; p.budget = budget; p.n_sink = n_sink; p.n_recent = n_recent;
   p.per_head = per_head != 0; p.dst_table = dst_table_dev; p.dst_blocks = dst_blocks;
   p.kept = kept_out_dev; p.new_len = new_len_out_dev; p.n_keep = h->n_keep;
-  ILRE_CUDA(launch_evict(p, h->n_sm, st));
+  if (dst_table_dev && evict_copy_blocks(p) > 2147483647LL) return ILRE_ERR_CAPACITY;
+  ILRE_CUDA(launch_evict(p, st));
   h->last_launches = 2;
   return ILRE_OK;
 }

@@ -35,6 +35,10 @@ struct PagedAttnParams {
   ChunkJoin* join;                               // [CTA]
 };
 
+// Shared memory of the kernels, once per device.
+cudaError_t init_paged_rows();
+cudaError_t init_paged_chunk();
+
 // map_k, map_v: the pools as {channel, kv head, row, page}, boxes of 64 channels x min(page_size, kRowKeys) rows.
 cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v, const PagedAttnParams& p, bool f16,
                               int n_sm, cudaStream_t st);

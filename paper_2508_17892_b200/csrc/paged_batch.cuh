@@ -249,7 +249,7 @@ struct Piece {
 // The pieces of a CTA's share: the last one first, then the others in order.  The last piece begins at its item's
 // first keys and the first one usually goes on where another CTA's stops, so that in this order the CTAs that work
 // on query tiles of one sequence pass over its keys side by side, and one of them brings each key tile into L2 for
-// all (1024 tokens behind 31744 rows: ORDER_US).
+// all (1024 tokens behind 31744 rows: in the order of the units 588 us, so 480).
 template <class Tiles>
 struct PieceWalk {
   long long u, end;                        // units that follow the current piece

@@ -566,13 +566,17 @@ paged_join_kernel(const __grid_constant__ PagedAttnParams p, int tok) {
 
 }  // namespace
 
+cudaError_t init_paged_chunk() {
+  const cudaError_t e = cudaFuncSetAttribute(paged_chunk_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(paged_chunk_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+}
+
 cudaError_t launch_paged_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                const PagedAttnParams& p, bool f16, int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-  if (e != cudaSuccess) return e;
   const TileShape ts = {p.n_kv, 2 * (128 / p.group), 7};
-  e = launch_after_previous(k, n_sm, kThreads, kSmem, st, map_q, map_k, map_v, p, ts);
+  const cudaError_t e = launch_after_previous(k, n_sm, kThreads, kSmem, st, map_q, map_k, map_v, p, ts);
   if (e != cudaSuccess) return e;
   auto j = f16 ? paged_join_kernel<true> : paged_join_kernel<false>;
   return launch_after_previous(j, dim3(n_sm, 128 / kJoinChannels), kChunkRows, 0, st, p, 128 / p.group);

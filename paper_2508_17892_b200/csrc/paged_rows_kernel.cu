@@ -349,11 +349,15 @@ constexpr size_t kSmem = kStages * kStageBytes + 2 * kMergeFloats * 4 + sizeof(R
 
 }  // namespace
 
+cudaError_t init_paged_rows() {
+  const cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(paged_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+}
+
 cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v, const PagedAttnParams& p, bool f16,
                               int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_rows_kernel<true> : paged_rows_kernel<false>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-  if (e != cudaSuccess) return e;
   // a column of work: up to 16 heads of a kv head's group
   RowShape rs;
   rs.hs = p.group < kRowTile ? p.group : kRowTile;

@@ -391,11 +391,15 @@ int weight_tile_tokens(int group, int max_q_len) {
   return max_q_len < most ? (max_q_len < 1 ? 1 : max_q_len) : most;
 }
 
+cudaError_t init_paged_weights() {
+  const cudaError_t e = cudaFuncSetAttribute(paged_weights_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(paged_weights_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+}
+
 cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& map_k, const PagedWeightParams& p, bool f16,
                                  int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_weights_kernel<true> : paged_weights_kernel<false>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-  if (e != cudaSuccess) return e;
   const TileShape ts = {p.n_kv, weight_tile_tokens(p.group, p.batch.max_q_len), 7};
   const int rows = ts.tq * p.group;
   WeightRings r;

@@ -35,6 +35,11 @@ struct EvictParams {
   int32_t* n_keep;                               // workspace [max_seqs]: rows that stay, -1: sequence left out
 };
 
+// Shared memory of the kernels, once per device.
+cudaError_t init_paged_weights();
+cudaError_t init_paged_weight_rows();
+cudaError_t init_evict();
+
 // Query tokens of a row tile: 128 rows, or all that any sequence has.
 int weight_tile_tokens(int group, int max_q_len);
 // map_q: {channel, head, token}, boxes of 64 channels x group x weight_tile_tokens; map_k: the pool as {channel, kv head,
@@ -44,6 +49,7 @@ cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& ma
 // Sequences of at most 16 rows (new tokens x heads of a group).
 cudaError_t launch_paged_weight_rows(const CUtensorMap& map_k, const PagedWeightParams& p, bool f16, int n_sm,
                                      cudaStream_t st);
-cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st);
+long long evict_copy_blocks(const EvictParams& p);     // CTAs per sequence of the copy to other pages, < 2^31
+cudaError_t launch_evict(const EvictParams& p, cudaStream_t st);
 
 }  // namespace ilre

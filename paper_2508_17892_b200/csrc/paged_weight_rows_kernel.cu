@@ -187,10 +187,14 @@ constexpr size_t kSmem = kStages * kStageBytes + sizeof(Tail);
 
 }  // namespace
 
+cudaError_t init_paged_weight_rows() {
+  const cudaError_t e = cudaFuncSetAttribute(paged_weight_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(paged_weight_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+}
+
 cudaError_t launch_paged_weight_rows(const CUtensorMap& map_k, const PagedWeightParams& p, bool f16, int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_weight_rows_kernel<true> : paged_weight_rows_kernel<false>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-  if (e != cudaSuccess) return e;
   const TileShape ts = {p.n_kv, 16 / p.group, 7};
   return launch_after_previous(k, 2 * n_sm, kThreads, kSmem, st, map_k, p, ts);
 }

@@ -70,9 +70,11 @@ class RopeSpec:
     high: float = 4.0
     attn_factor: float = 0.0
 
-    def c_struct(self) -> IlreRopeSpec:
-        return IlreRopeSpec(self.theta, self.rotary_dim, int(self.interleaved), _SCALINGS[self.scaling], self.factor,
-                            self.orig_len, self.low, self.high, self.attn_factor)
+    def __post_init__(self):
+        object.__setattr__(self, "_c", IlreRopeSpec(
+            self.theta, self.rotary_dim, int(self.interleaved), _SCALINGS[self.scaling], self.factor, self.orig_len,
+            self.low, self.high, self.attn_factor))
+        object.__setattr__(self, "ref", ctypes.byref(self._c))
 
 
 @dataclass(frozen=True)
@@ -84,10 +86,11 @@ class PagedBatch:
     n_tokens: int
     max_q_len: int
 
-    def c_struct(self) -> IlrePagedBatch:
-        return IlrePagedBatch(self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1],
-                              self.q_start.data_ptr() if self.q_start is not None else None, self.kv_len.data_ptr(),
-                              self.block_table.data_ptr())
+    def __post_init__(self):
+        object.__setattr__(self, "_c", IlrePagedBatch(
+            self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1], _ptr(self.q_start),
+            self.kv_len.data_ptr(), self.block_table.data_ptr()))
+        object.__setattr__(self, "ref", ctypes.byref(self._c))
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -96,29 +99,34 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _rows(t: torch.Tensor, device, dtype, heads: int, dim: int) -> int:
     """Stride in elements from token to token of a tensor [n, heads, dim] whose tokens are contiguous."""
-    assert t.device == device and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, dim)
-    assert t.shape[0] == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim))
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+    assert t.device == device and t.dtype == dtype and t.dim() == 3
+    (n, h, d), (st, sh, sd) = t.shape, t.stride()
+    assert h == heads and d == dim and (n == 0 or (sd == 1 and (heads == 1 or sh == dim)))
+    return st if n > 1 else heads * dim
 
 
 class _OnStream:
-    """The stream of a call: its device is current inside, tensors made inside are its own, and the caller's
-    tensors are marked as in use by it."""
+    """The stream of a call.  Where the caller names one, tensors made inside are its own and the caller's
+    tensors are marked as in use by it; without a name it is the device's current one."""
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], tensors):
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        if stream is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        self._ctx = torch.cuda.stream(self.stream)
+        self._ctx = None
+        if stream is None:
+            self.raw = torch._C._cuda_getCurrentRawStream(device.index)       # (a Stream object takes microseconds)
+            return
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        self.raw = stream.cuda_stream
+        self._ctx = torch.cuda.stream(stream)
 
     def __enter__(self):
-        self._ctx.__enter__()
-        return self.stream.cuda_stream
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        return self.raw
 
     def __exit__(self, *exc):
-        return self._ctx.__exit__(*exc)
+        return self._ctx.__exit__(*exc) if self._ctx is not None else None
 
 
 def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: bool = False,
@@ -137,8 +145,13 @@ def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: b
             out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
         out_stride = _rows(out, x.device, x.dtype, heads, dim)
         assert out.shape[0] == n
-        rc = load_library().ilre_rope(ctypes.byref(spec.c_struct()), x.data_ptr(), x_stride, out.data_ptr(), out_stride,
-                                      positions.data_ptr(), n, heads, dim, _DTYPES[x.dtype], int(transposed), st)
+        args = (spec.ref, x.data_ptr(), x_stride, out.data_ptr(), out_stride, positions.data_ptr(), n, heads, dim,
+                _DTYPES[x.dtype], int(transposed), st)
+        if torch.cuda.current_device() == x.device.index:
+            rc = load_library().ilre_rope(*args)
+        else:
+            with torch.cuda.device(x.device):
+                rc = load_library().ilre_rope(*args)
     if rc != 0:
         raise IlreError(rc, "ilre_rope")
     return out
@@ -160,8 +173,10 @@ class PagedCache:
         if rc != 0:
             self._h = ctypes.c_void_p()
             raise IlreError(rc, "ilre_paged_create")
-        self.dtype = dtype
+        self.dtype, self._n_q, self._dim = dtype, n_q_heads, head_dim
         self.device = torch.device("cuda", device)
+        self._page_shape = (page_size, n_kv_heads, head_dim)
+        self._page_stride = (n_kv_heads * head_dim, head_dim, 1)
 
     def batch(self, q_start: Optional[torch.Tensor], kv_len: torch.Tensor, block_table: torch.Tensor, n_tokens: int,
               max_q_len: int) -> PagedBatch:
@@ -174,19 +189,24 @@ class PagedCache:
         return PagedBatch(q_start, kv_len, block_table, n_tokens, max_q_len)
 
     def _pool(self, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
-        c = self.cfg
-        for t in (k, v):
-            assert t is None or (t.device == self.device and t.dtype == self.dtype and t.dim() == 4 and
-                                 t.shape == (k.shape[0], c.page_size, c.n_kv_heads, c.head_dim) and
-                                 (t.shape[0] == 0 or t[0].is_contiguous()))
+        c, n_pages = self.cfg, k.shape[0]
+        page = self._page_shape
+
+        def stride(t):
+            if t is None:
+                return 0
+            assert t.device == self.device and t.dtype == self.dtype and t.shape == (n_pages,) + page
+            first, rest = t.stride()[0], t.stride()[1:]
+            assert n_pages == 0 or rest == self._page_stride or t[0].is_contiguous()
+            return first if n_pages > 1 else 0
+
         assert w is None or (w.device == self.device and w.dtype == torch.float32 and w.is_contiguous() and
-                             w.shape == (k.shape[0], c.n_kv_heads, c.page_size))
-        stride = lambda t: t.stride(0) if t is not None and t.shape[0] > 1 else 0  # noqa: E731
-        return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), stride(k), stride(v), k.shape[0])
+                             w.shape == (n_pages, c.n_kv_heads, c.page_size))
+        return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), stride(k), stride(v), n_pages)
 
     def _q(self, batch: PagedBatch, q: torch.Tensor) -> int:
         assert q.shape[0] == batch.n_tokens and (batch.n_tokens == 0 or batch.q_start is not None)
-        return _rows(q, self.device, self.dtype, self.cfg.n_q_heads, self.cfg.head_dim)
+        return _rows(q, self.device, self.dtype, self._n_q, self._dim)
 
     def _check(self, rc: int, what: str) -> None:
         if rc != 0:
@@ -219,7 +239,7 @@ class PagedCache:
             else:
                 assert q_out is None
             self._check(self._lib.ilre_paged_append(
-                self._h, ctypes.byref(batch.c_struct()), ctypes.byref(spec.c_struct()) if spec is not None else None,
+                self._h, batch.ref, spec.ref if spec is not None else None,
                 _ptr(positions), _ptr(q), q_stride, _ptr(q_out), q_out_stride, k.data_ptr(), k_stride, v.data_ptr(),
                 v_stride, ctypes.byref(pool), st), "ilre_paged_append")
         return q_out
@@ -242,7 +262,7 @@ class PagedCache:
             assert out.shape == (batch.n_tokens, c.n_q_heads, c.head_dim)
             self._lse(batch, lse)
             self._check(self._lib.ilre_paged_attention(
-                self._h, ctypes.byref(batch.c_struct()), q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
+                self._h, batch.ref, q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
                 _ptr(lse), st), "ilre_paged_attention")
         return out, lse
 
@@ -261,7 +281,7 @@ class PagedCache:
         with _OnStream(self.device, stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len,
                                              batch.block_table)) as st:
             self._check(self._lib.ilre_paged_accumulate(
-                self._h, ctypes.byref(batch.c_struct()), q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
+                self._h, batch.ref, q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
                 st), "ilre_paged_accumulate")
         return w_pool
 
@@ -289,7 +309,7 @@ class PagedCache:
             for t, want in ((kept, shape), (new_len, (n,))):
                 assert t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and t.shape == want
             self._check(self._lib.ilre_paged_evict(
-                self._h, ctypes.byref(batch.c_struct()), budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
+                self._h, batch.ref, budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
                 _ptr(dst_table), dst_table.shape[1] if dst_table is not None else 0, kept.data_ptr(),
                 new_len.data_ptr(), st), "ilre_paged_evict")
         return kept, new_len
