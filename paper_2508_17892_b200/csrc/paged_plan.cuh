@@ -57,10 +57,34 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
   }
 }
 
+// The same for a batch of at most 32 sequences: one load of the lengths and no barrier, each of two warps for itself.
+template <class Tiles>
+__device__ __forceinline__ void plan_small(const PagedBatch& b, const TileShape& ts, int min_units, PlanStart* out) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (warp >= 2) return;
+  const long long n = lane < b.n_seqs ? seq_units<Tiles>(b, ts, lane) : 0;
+  long long incl = n;
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  const long long total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+  const int n_cta = share_ctas(total, gridDim.x, min_units), c = blockIdx.x;
+  const bool has = total > 0 && c < n_cta;
+  const long long u0 = has ? share_begin(total, n_cta, c) : 0, u1 = has ? share_begin(total, n_cta, c + 1) : 0;
+  if (threadIdx.x == 0) { out->total = total; out->n_cta = n_cta; out->u0 = u0; out->u1 = u1; }
+  if (!has) return;
+  const long long at = warp ? u1 - 1 : u0, begin = incl - n;
+  const int seq = __ffs(__ballot_sync(0xFFFFFFFFu, begin <= at && at < incl)) - 1;
+  const Item x = locate<Tiles>(b, ts, seq, __shfl_sync(0xFFFFFFFFu, begin, seq), at);
+  if (lane == 0) { if (warp) out->last = x; else out->first = x; }
+}
+
 // This CTA's share: all threads; *out is valid behind the next barrier.
 template <class Tiles>
 __device__ __forceinline__ void plan_start(const PagedBatch& b, const TileShape& ts, int min_units, long long* tmp,
                                            PlanStart* out) {
+  if (b.n_seqs <= 32) return plan_small<Tiles>(b, ts, min_units, out);
   long long mine;
   const long long total = plan_total<Tiles>(b, ts, tmp, &mine);
   const int n_cta = share_ctas(total, gridDim.x, min_units), c = blockIdx.x;

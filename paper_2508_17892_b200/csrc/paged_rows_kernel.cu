@@ -287,13 +287,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const int b_first = share_of(plan.total, plan.n_cta, pc.item);
       const int b_last = share_of(plan.total, plan.n_cta, pc.item + pc.n_tiles - 1);
       if (warp == 0) {
-        __threadfence();
         __syncwarp();
-        if (lane == 0) {                                 // wraps to 0 with the last arrival
-          const int n = b_last - b_first + 1;
-          tail->last = atomicInc(p.arrived + b_first, n - 1) == static_cast<uint32_t>(n - 1);
-          __threadfence();
-        }
+        if (lane == 0) tail->last = arrive_last(p.arrived + b_first, b_last - b_first + 1);
       }
       sync_consumers();
       if (tail->last && ok) {

@@ -345,13 +345,9 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           const Item& x = (job.flags & kOfFirst) ? plan.first : plan.last;
           const int c0 = share_of(plan.total, plan.n_cta, x.begin), c1 = share_of(plan.total, plan.n_cta, x.begin + x.n_tiles - 1);
           p.part[(blockIdx.x * 2 + (blockIdx.x == c0)) * 128 + key_lane] = sum;
-          __threadfence();
           ok = agree(group, ok);
           if (!ok) break;
-          if (gi == 0) {                                 // wraps to 0 with the last arrival
-            tail->last[group] = atomicInc(p.arrived + c0, c1 - c0) == static_cast<uint32_t>(c1 - c0);
-            __threadfence();
-          }
+          if (gi == 0) tail->last[group] = arrive_last(p.arrived + c0, c1 - c0 + 1);
           ok = agree(group, ok);
           if (!ok) break;
           write = tail->last[group] != 0;

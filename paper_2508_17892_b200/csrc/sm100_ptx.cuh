@@ -325,6 +325,14 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
+// One more arrival on a counter that wraps to 0 with the last of `n`; true for the last.  What the threads that this
+// one has synchronised with wrote before is visible to the last one's threads behind their next barrier.
+__device__ __forceinline__ bool arrive_last(uint32_t* count, uint32_t n) {
+  uint32_t old;
+  asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(count), "r"(n - 1) : "memory");
+  return old == n - 1;
+}
+
 // ---- programmatic dependent launch ----
 // A kernel launched with the programmatic-stream-serialization attribute may start while the
 // kernel before it in the stream still runs, once every CTA of that kernel has called
