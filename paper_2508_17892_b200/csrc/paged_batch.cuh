@@ -14,8 +14,11 @@ namespace ilre {
 // One head of one sequence: n query tokens in tiles of `tq`, the last of them seeing all kv rows, keys in tiles
 // of 2^tk_shift.  Every query tile has at least one key tile (a tile that sees nothing still writes its output).
 // Lengths stay below 2^31 - 2048, so what a tile sees fits 32 bits; sums take 64.
+//
+// An item costs more than its key tiles (its queries arrive, its output leaves): `extra` units in front of them stand
+// for that, so that CTAs with many short items get fewer tiles.
 struct HeadTiles {
-  int n, kv, tq, tk_shift;
+  int n, kv, tq, tk_shift, extra;
   __host__ __device__ int n_qt() const { return n <= tq ? (n > 0) : static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   __host__ __device__ int key_tiles(int qt) const {
     const long long last = static_cast<long long>(qt + 1) * tq;
@@ -28,7 +31,7 @@ struct HeadTiles {
   __host__ __device__ long long before(int qt) const {
     const int pre = kv - n;
     int blind = pre < 0 ? static_cast<int>(static_cast<unsigned>(-pre) / tq) : 0;        // tiles that see nothing
-    if (blind >= qt) return qt;
+    if (blind >= qt) return static_cast<long long>(qt) * (1 + extra);
     const unsigned b = static_cast<unsigned>(pre + (blind + 1) * tq) + (1u << tk_shift) - 1;
     int z = 0;
     while (z < tk_shift && !((tq >> z) & 1)) ++z;
@@ -41,12 +44,12 @@ struct HeadTiles {
       whole += f;
       if (i < r) rest += f;
     }
-    return blind + k * whole + s * P * (k * (k - 1) / 2) + rest + s * k * r;
+    return blind + k * whole + s * P * (k * (k - 1) / 2) + rest + s * k * r + static_cast<long long>(qt) * extra;
   }
   __host__ __device__ long long units() const {
     if (n <= 0) return 0;
     const int last = n_qt() - 1;
-    return before(last) + key_tiles(last);
+    return before(last) + key_tiles(last) + extra;
   }
   // the query tile that unit u of this head belongs to: the largest qt with before(qt) <= u
   __host__ __device__ int tile_of(long long u) const {
@@ -63,7 +66,7 @@ struct HeadTiles {
 // the tiles of `tq` query tokens that see any of them.  (The names are HeadTiles': "query tile" is the item's
 // number, "key tiles" are its units.)
 struct KeyTiles {
-  int n, kv, tq, tk_shift;
+  int n, kv, tq, tk_shift, extra;          // extra: 0
   __host__ __device__ int n_qt() const { return static_cast<int>((static_cast<unsigned>(kv) + (1u << tk_shift) - 1) >> tk_shift); }
   __host__ __device__ int row_tiles() const { return n <= tq ? 1 : static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   // the first row tile that sees a key of tile kt
@@ -178,14 +181,14 @@ __host__ __device__ __forceinline__ int page_of(const PagedBatch& b, int seq, in
 
 // Tiles of the batch's heads: `heads` work columns per sequence (kv heads, or parts of their groups).
 struct TileShape {
-  int heads, tq, tk_shift;
+  int heads, tq, tk_shift, extra;
 };
 
 template <class Tiles>
 __host__ __device__ __forceinline__ long long seq_units(const PagedBatch& b, const TileShape& ts, int i) {
   const SeqSpan s = load_span(b, i);
   if (!in_range(b, s.n)) return 0;
-  return Tiles{s.n, s.kv, ts.tq, ts.tk_shift}.units() * ts.heads;
+  return Tiles{s.n, s.kv, ts.tq, ts.tk_shift, ts.extra}.units() * ts.heads;
 }
 
 // The query tile of one head that a unit lies in.
@@ -193,6 +196,8 @@ struct Item {
   SeqSpan span;
   int seq, head, qt, n_tiles;              // n_tiles: key tiles
   long long begin;                         // its first unit
+  __host__ __device__ long long tiles_at(const TileShape& ts) const { return begin + ts.extra; }
+  __host__ __device__ long long end(const TileShape& ts) const { return begin + ts.extra + n_tiles; }
 };
 
 // The query tile of a head's unit.  On the device all lanes of a warp ask together and try 32 tiles at a time.
@@ -221,7 +226,7 @@ __host__ __device__ __forceinline__ Item locate(const PagedBatch& b, const TileS
   Item x;
   x.seq = seq;
   x.span = load_span(b, seq);
-  const Tiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift};
+  const Tiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift, ts.extra};
   const long long per_head = tiles.units(), off = at - seq_begin;
   x.head = static_cast<int>(div_pos(off, per_head));
   const long long in_head = off - x.head * per_head;
@@ -257,50 +262,51 @@ struct PieceWalk {
   int n_qt;
   Piece p;
 
-  // Positions on the first piece; false if the share is empty.
-  __host__ __device__ __forceinline__ bool begin(const TileShape& ts, const PlanStart& s) {
+  // Positions on the first piece; false if the share has none.
+  __host__ __device__ __forceinline__ bool begin(const PagedBatch& b, const TileShape& ts, const PlanStart& s) {
     if (s.u0 >= s.u1) return false;
     last = true;
     end = s.u1;
-    open(ts, s.last, s.last.begin < s.u0 ? static_cast<int>(s.u0 - s.last.begin) : 0);
-    return true;
+    return open(ts, s.last, s.last.begin < s.u0 ? s.u0 : s.last.begin) || next(b, ts, s);
   }
-  __host__ __device__ __forceinline__ void open(const TileShape& ts, const Item& x, int t0) {
+  // The item from unit `at` on; false if the share has none of its tiles.
+  __host__ __device__ __forceinline__ bool open(const TileShape& ts, const Item& x, long long at) {
     p.span = x.span; p.seq = x.seq; p.head = x.head; p.qt = x.qt; p.n_tiles = x.n_tiles; p.item = x.begin;
-    p.t0 = t0;
-    n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
-    close();
+    n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.n_qt();
+    return close(ts, at);
   }
-  __host__ __device__ __forceinline__ void close() {
-    const long long left = end - p.item;
-    p.t1 = left < p.n_tiles ? static_cast<int>(left) : p.n_tiles;
-    u = p.item + p.t1;
+  __host__ __device__ __forceinline__ bool close(const TileShape& ts, long long at) {
+    const long long from = at - p.item - ts.extra, left = end - p.item - ts.extra;
+    p.t0 = from > 0 ? static_cast<int>(from) : 0;
+    p.t1 = left < 0 ? 0 : left < p.n_tiles ? static_cast<int>(left) : p.n_tiles;
+    u = p.item + ts.extra + p.n_tiles;
+    if (u > end) u = end;
+    return p.t0 < p.t1;
   }
   __host__ __device__ __forceinline__ bool next(const PagedBatch& b, const TileShape& ts, const PlanStart& s) {
     if (last) {
       last = false;
       end = s.last.begin;
       if (s.u0 >= end) return false;
-      open(ts, s.first, static_cast<int>(s.u0 - s.first.begin));
-      return true;
+      if (open(ts, s.first, s.u0)) return true;
     }
-    if (u >= end) return false;
-    if (++p.qt == n_qt) {
-      p.qt = 0;
-      if (++p.head == ts.heads) {
-        p.head = 0;
-        do {                               // units are left, so a sequence with work follows
-          if (++p.seq >= b.n_seqs) return false;
-          p.span = load_span(b, p.seq);
-        } while (!in_range(b, p.span.n) || Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.units() == 0);
-        n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.n_qt();
+    while (u < end) {
+      if (++p.qt == n_qt) {
+        p.qt = 0;
+        if (++p.head == ts.heads) {
+          p.head = 0;
+          do {                             // units are left, so a sequence with work follows
+            if (++p.seq >= b.n_seqs) return false;
+            p.span = load_span(b, p.seq);
+          } while (!in_range(b, p.span.n) || Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.units() == 0);
+          n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.n_qt();
+        }
       }
+      p.item = u;
+      p.n_tiles = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.key_tiles(p.qt);
+      if (close(ts, u)) return true;
     }
-    p.t0 = 0;
-    p.item = u;
-    p.n_tiles = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift}.key_tiles(p.qt);
-    close();
-    return true;
+    return false;
   }
 };
 

@@ -29,6 +29,7 @@ constexpr int kThreads = 352;                            // warp 0 loads, 1 S MM
 constexpr int kSoftmaxWarps = 4;
 constexpr int kPolyPairs = 2;                            // of 16 pairs of exponentials, those on the FMA pipe
 constexpr int kEarly = 2;                                // of a tile's four groups, those before the wait for P
+constexpr int kItemUnits = 3;                            // what an item costs beside its tiles, in tiles
 constexpr int kMinUnits = 2;                             // 128-key tiles that a CTA gets at least
 
 struct ChunkTail {
@@ -109,8 +110,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   if (threadIdx.x == 0) {                                // the item that begins here and goes on in other shares
     const PlanStart& s = tail->plan;
     ChunkJoin j = {-1, 0, 0, 0};
-    if (s.u0 < s.u1 && s.last.begin >= s.u0 && s.last.begin + s.last.n_tiles > s.u1) {
-      j.c_last = share_of(s.total, s.n_cta, s.last.begin + s.last.n_tiles - 1);
+    if (s.u0 < s.u1 && s.last.tiles_at(ts) >= s.u0 && s.last.tiles_at(ts) < s.u1 && s.last.end(ts) > s.u1) {
+      j.c_last = share_of(s.total, s.n_cta, s.last.end(ts) - 1);
       j.token = s.last.span.q0 + s.last.qt * ts.tq;
       j.n_tok = min(ts.tq, s.last.span.n - s.last.qt * ts.tq);
       j.head = s.last.head;
@@ -133,7 +134,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const bool active = bx < n_box;
     const uint32_t off = half * kHalf + bx * box_rows * 128;
     PieceWalk<HeadTiles> w;
-    bool ok = run && w.begin(ts, tail->plan), more = ok;
+    bool ok = run && w.begin(b, ts, tail->plan), more = ok;
     int it = 0, n_piece = 0;
     while (more && ok) {
       const Piece& pc = w.p;
@@ -194,7 +195,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       const bool s_role = (warp == 1);
       volatile int* v_landed = &tail->v_landed;
       PieceWalk<HeadTiles> w;
-      bool ok = w.begin(ts, tail->plan), more = ok;
+      bool ok = w.begin(b, ts, tail->plan), more = ok;
       int it0 = 0, tile0 = 0, n_prev = 2, n_piece = 0;
       uint32_t done[2] = {0, 0};                         // tiles of each stream so far
       int landed = 0;
@@ -304,7 +305,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     uint32_t items = 0;                                  // ring items before this piece
     bool ok = run;
     bool more;
-    if (lane == 0) more = walk->begin(ts, tail->plan);
+    if (lane == 0) more = walk->begin(b, ts, tail->plan);
     more = __shfl_sync(0xFFFFFFFFu, more, 0);
     __syncwarp();
     while (more && ok) {
@@ -434,7 +435,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           if (walk->p.t0 == 0 && walk->p.t1 == walk->p.n_tiles) {
             // O / sum through this warp's rows of the P buffer (its MMAs are done), out in whole rows of 256 bytes
             const float inv_l = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
+#pragma unroll 2
             for (int q4 = 0; q4 < 4; ++q4) {
               float v[32];
               tmem_ld32(o_tm + q4 * 32, v);
@@ -449,12 +450,23 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             tc_fence_before();
             __syncwarp();
-            const int c16 = lane & 15;
-            for (int r = quad * 32 + (lane >> 4); r < quad * 32 + 32; r += 2) {
-              const int rt = r / p.group, rh = r - rt * p.group;
-              if (rt < valid_tok) {
-                const uint4 v = *reinterpret_cast<const uint4*>(p_mine + (c16 >> 3) * kHalf + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
-                static_cast<uint4*>(p.out)[((tok_at + rt) * p.n_q + head0 + rh) * 16 + c16] = v;
+            const int c16 = lane & 15, row0 = quad * 32 + (lane >> 4), step_t = 2 / p.group, step_h = 2 - step_t * p.group;
+            int rt = row0 / p.group, rh = row0 - rt * p.group;
+            uint4* dst = static_cast<uint4*>(p.out) + (tok_at * p.n_q + head0) * 16 + c16;
+#pragma unroll
+            for (int r8 = 0; r8 < 2; ++r8) {
+              uint4 v[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int r = row0 + 2 * (r8 * 8 + k);
+                v[k] = *reinterpret_cast<const uint4*>(p_mine + (c16 >> 3) * kHalf + r * 128 + (((c16 & 7) ^ (r & 7)) << 4));
+              }
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                if (rt < valid_tok) dst[(static_cast<long long>(rt) * p.n_q + rh) * 16] = v[k];
+                rt += step_t;
+                rh += step_h;
+                if (rh >= p.group) { rh -= p.group; ++rt; }
               }
             }
             __syncwarp();
@@ -575,7 +587,7 @@ cudaError_t init_paged_chunk() {
 cudaError_t launch_paged_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                const PagedAttnParams& p, bool f16, int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
-  const TileShape ts = {p.n_kv, 2 * (128 / p.group), 7};
+  const TileShape ts = {p.n_kv, 2 * (128 / p.group), 7, kItemUnits};
   const cudaError_t e = launch_after_previous(k, n_sm, kThreads, kSmem, st, map_q, map_k, map_v, p, ts);
   if (e != cudaSuccess) return e;
   auto j = f16 ? paged_join_kernel<true> : paged_join_kernel<false>;

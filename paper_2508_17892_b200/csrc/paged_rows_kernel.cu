@@ -76,7 +76,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   __syncthreads();
   const PlanStart& plan = tail->plan;
   PieceWalk<HeadTiles> w;
-  if (!w.begin(ts, plan)) return;
+  if (!w.begin(b, ts, plan)) return;
   bool ok = *abort_flag == 0;
 
   if (warp == kWarps) {
@@ -357,7 +357,7 @@ cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v
   RowShape rs;
   rs.hs = p.group < kRowTile ? p.group : kRowTile;
   rs.parts = (p.group + rs.hs - 1) / rs.hs;
-  const TileShape ts = {p.n_kv * rs.parts, kRowTile / rs.hs, 6};
+  const TileShape ts = {p.n_kv * rs.parts, kRowTile / rs.hs, 6, 0};
   return launch_after_previous(k, n_sm * kRowCtasPerSm, kThreads, kSmem, st, map_k, map_v, p, ts, rs);
 }
 

@@ -165,7 +165,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const bool active = bx < n_box;
     const uint32_t off = half * kHalf + bx * box_rows * 128;
     PieceWalk<KeyTiles> w;
-    bool more = ok && w.begin(ts, plan);
+    bool more = ok && w.begin(b, ts, plan);
     int n_key = 0, n_row = 0;
     RingPos kp, qp;
     auto publish = [&](const Job& job) {
@@ -187,7 +187,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       e_next = needs(next_kt, pc) ? table_entry(b, pc.seq, next_kt * 128 + bx * box_rows) : 0;
       ok = warp_wait(&tail->k_empty[kp.slot], kp.phase ^ 1u, abort_flag, b.status, kDevWaitKEmpty);
       if (!ok) break;
-      const int r_first = KeyTiles{pc.span.n, pc.span.kv, ts.tq, ts.tk_shift}.first(pc.qt) + pc.t0;
+      const int r_first = KeyTiles{pc.span.n, pc.span.kv, ts.tq, ts.tk_shift, 0}.first(pc.qt) + pc.t0;
       const bool cut = pc.t0 > 0 || pc.t1 < pc.n_tiles;
       publish(Job{pc.qt, r_first, pc.t1 - pc.t0, (cut ? kCut : 0) | (pc.item == plan.first.begin ? kOfFirst : 0), pc.span.q0,
                   pc.span.n, pc.span.kv, pc.head + p.n_kv * pc.seq});
@@ -396,7 +396,7 @@ cudaError_t init_paged_weights() {
 cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& map_k, const PagedWeightParams& p, bool f16,
                                  int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_weights_kernel<true> : paged_weights_kernel<false>;
-  const TileShape ts = {p.n_kv, weight_tile_tokens(p.group, p.batch.max_q_len), 7};
+  const TileShape ts = {p.n_kv, weight_tile_tokens(p.group, p.batch.max_q_len), 7, 0};
   const int rows = ts.tq * p.group;
   WeightRings r;
   r.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;

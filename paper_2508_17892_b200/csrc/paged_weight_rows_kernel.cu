@@ -57,7 +57,7 @@ paged_weight_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
   plan_start<HeadTiles>(b, ts, 1, tail->tmp, &tail->plan);
   __syncthreads();
   PieceWalk<HeadTiles> w;
-  bool more = *abort_flag == 0 && w.begin(ts, tail->plan), ok = more;
+  bool more = *abort_flag == 0 && w.begin(b, ts, tail->plan), ok = more;
 
   if (warp == kWarps) {
     const int ps = 1 << b.page_shift;
@@ -195,7 +195,7 @@ cudaError_t init_paged_weight_rows() {
 
 cudaError_t launch_paged_weight_rows(const CUtensorMap& map_k, const PagedWeightParams& p, bool f16, int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_weight_rows_kernel<true> : paged_weight_rows_kernel<false>;
-  const TileShape ts = {p.n_kv, 16 / p.group, 7};
+  const TileShape ts = {p.n_kv, 16 / p.group, 7, 0};
   return launch_after_previous(k, 2 * n_sm, kThreads, kSmem, st, map_k, p, ts);
 }
 

@@ -20,11 +20,13 @@ static int bad = 0;
 
 const int tqs[] = {1, 2, 4, 16, 50, 64, 256}, tks[] = {6, 7};
 struct Q : HeadTiles {
-  Q(int n, int kv, int tq, int tk) : HeadTiles{n, kv, tq, tk} {}
+  Q(int n, int kv, int tq, int tk, int extra) : HeadTiles{n, kv, tq, tk, extra} {}
+  static constexpr bool kExtra = true;
   static bool counts(int) { return true; }
 };
 struct K : KeyTiles {
-  K(int n, int kv, int tq, int tk) : KeyTiles{n, kv, tq, tk} {}
+  K(int n, int kv, int tq, int tk, int extra) : KeyTiles{n, kv, tq, tk, extra} {}
+  static constexpr bool kExtra = false;
   static bool counts(int kv) { return kv > 0; }
 };
 
@@ -46,7 +48,7 @@ void batches(std::mt19937& rng) {
     int status = 0;
     PagedBatch b{n, pick(0, 5) ? q_start[n] : q_start[n] + 3, max_q, max_blocks, page_shift, 1, 0, 1 << 30, q_start.data(), kv.data(),
                  table.data(), &status};
-    const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2]};
+    const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2], Tiles::kExtra ? pick(0, 3) : 0};
     std::vector<long long> units(n), begin(n + 1, 0);
     for (int i = 0; i < n; ++i) {
       const long long len = static_cast<long long>(q_start[i + 1]) - q_start[i];
@@ -62,12 +64,13 @@ void batches(std::mt19937& rng) {
     const int grid = pick(1, 60), n_cta = share_ctas(total, grid, pick(1, 4));
     CHECK(n_cta >= 1 && n_cta <= grid);
     long long u = 0;
-    int seq = -1, head = 0, qt = 0, tile = 0;
+    int seq = -1, head = 0, qt = 0, tile = 0, c_begin = 0;
     for (int c = 0; c < n_cta; ++c) {
       PlanStart s;
       s.total = total; s.n_cta = n_cta;
       s.u0 = share_begin(total, n_cta, c); s.u1 = share_begin(total, n_cta, c + 1);
       CHECK(s.u0 == u && s.u1 > s.u0);
+      u = s.u1;
       int a = 0, z = 0;
       while (begin[a + 1] <= s.u0) ++a;
       while (begin[z + 1] < s.u1) ++z;
@@ -75,29 +78,35 @@ void batches(std::mt19937& rng) {
       s.last = locate<Tiles>(b, ts, z, begin[z], s.u1 - 1);
       PieceWalk<Tiles> w;
       std::vector<Piece> pieces;            // the last one comes first
-      for (bool more = w.begin(ts, s); more; more = w.next(b, ts, s)) pieces.push_back(w.p);
-      CHECK(pieces[0].item + pieces[0].t1 == s.u1);
-      std::rotate(pieces.begin(), pieces.begin() + 1, pieces.end());
+      for (bool more = w.begin(b, ts, s); more; more = w.next(b, ts, s)) pieces.push_back(w.p);
+      std::sort(pieces.begin(), pieces.end(), [](const Piece& x, const Piece& y) { return x.item < y.item; });
       for (const Piece& p : pieces) {
-        CHECK(p.t0 < p.t1 && p.t1 <= p.n_tiles && p.item + p.t0 == u);
+        CHECK(p.t0 < p.t1 && p.t1 <= p.n_tiles && p.item + ts.extra + p.t0 >= s.u0 && p.item + ts.extra + p.t1 <= s.u1);
         if (p.t0 == 0) {                    // a new item: the next in order
           CHECK(tile == 0);
           if (p.seq != seq) { CHECK(p.seq > seq && p.head == 0 && p.qt == 0); seq = p.seq; head = qt = 0; }
           CHECK(p.head == head && p.qt == qt);
+          c_begin = c;
+          // what the joining goes by
+          const Item x{p.span, p.seq, p.head, p.qt, p.n_tiles, p.item};
+          CHECK(share_of(total, n_cta, x.tiles_at(ts)) == c);
+          const bool listed = s.last.tiles_at(ts) >= s.u0 && s.last.tiles_at(ts) < s.u1 && s.last.end(ts) > s.u1;
+          CHECK((x.end(ts) > s.u1) == (listed && s.last.begin == p.item));
         } else {
-          CHECK(p.t0 == tile && p.seq == seq && p.head == head && p.qt == qt);
+          CHECK(p.t0 == tile && p.seq == seq && p.head == head && p.qt == qt && c > c_begin);
         }
-        CHECK(share_of(total, n_cta, p.item + p.t0) == c && share_of(total, n_cta, p.item + p.t1 - 1) == c);
-        u += p.t1 - p.t0;
+        CHECK(share_of(total, n_cta, p.item + ts.extra + p.t0) == c && share_of(total, n_cta, p.item + ts.extra + p.t1 - 1) == c);
         tile = p.t1 == p.n_tiles ? 0 : p.t1;
         if (tile == 0) {
-          Tiles h{p.span.n, p.span.kv, ts.tq, ts.tk_shift};
+          Tiles h{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra};
           if (++qt == h.n_qt()) { qt = 0; ++head; }
         }
       }
-      CHECK(u == s.u1);
     }
-    CHECK(u == total);
+    CHECK(u == total && tile == 0);
+    int last = n - 1;
+    while (units[last] == 0) --last;
+    CHECK(seq == last && head == ts.heads && qt == 0);
   }
 }
 
@@ -106,21 +115,21 @@ int main() {
   auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<unsigned>(hi - lo + 1)); };
   // one head: units, their prefix sums and the tile of each unit
   for (int i = 0; i < 4000; ++i) {
-    HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2]};
+    HeadTiles h{pick(1, 400), pick(0, 3) ? pick(0, 2000) : pick(0, 5), tqs[rng() % 7], tks[rng() % 2], pick(0, 1) * 3};
     long long at = 0;
     for (int qt = 0; qt < h.n_qt(); ++qt) {
       const int last = std::min((qt + 1) * h.tq, h.n), seen = h.kv - h.n + last;
       CHECK(h.key_tiles(qt) == (seen <= 0 ? 1 : (seen + (1 << h.tk_shift) - 1) >> h.tk_shift));
       CHECK(h.before(qt) == at);
-      for (long long u = at; u < at + h.key_tiles(qt); u += 3) CHECK(h.tile_of(u) == qt);
-      at += h.key_tiles(qt);
+      for (long long u = at; u < at + h.key_tiles(qt) + h.extra; u += 3) CHECK(h.tile_of(u) == qt);
+      at += h.key_tiles(qt) + h.extra;
     }
     CHECK(h.units() == at);
   }
   // the same from the keys: the row tiles that see a key of the tile
   const int tts[] = {1, 2, 3, 18, 25, 32, 42, 128};
   for (int i = 0; i < 4000; ++i) {
-    KeyTiles h{pick(1, 400), pick(1, 3) > 1 ? pick(1, 2000) : pick(1, 5), tts[rng() % 8], 7};
+    KeyTiles h{pick(1, 400), pick(1, 3) > 1 ? pick(1, 2000) : pick(1, 5), tts[rng() % 8], 7, 0};
     long long at = 0;
     for (int kt = 0; kt < h.n_qt(); ++kt) {
       int seen = 0;
@@ -136,10 +145,10 @@ int main() {
     CHECK(h.units() == at);
   }
   // far lengths: no overflow
-  HeadTiles far{1 << 30, 2147481000, 64, 7};
+  HeadTiles far{1 << 30, 2147481000, 64, 7, 3};
   CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
   CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
-  KeyTiles far_k{1 << 30, 2147481000, 18, 7};
+  KeyTiles far_k{1 << 30, 2147481000, 18, 7, 0};
   CHECK(far_k.tile_of(far_k.units() - 1) == far_k.n_qt() - 1 && far_k.key_tiles(far_k.n_qt() - 1) >= 1);
 
   batches<Q>(rng);
