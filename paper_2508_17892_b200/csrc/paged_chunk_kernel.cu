@@ -7,8 +7,9 @@
 // arrive in 128-key tiles through one TMA ring; a lane of the loading warp fetches the rows that one page has in the
 // tile.  The output is kept against a reference maximum that moves only when it is outrun by 2^8.
 //
-// What bounds it: the exponentials (one per logit, on the special-function units and partly as polynomials) and the
-// tensor pipe, of about the same length.  So nothing may leave either idle: the batch's key tiles are cut into
+// What bounds it: the exponentials (one per logit; a part of them as polynomials on the FMA pipe makes it slower, 431 ->
+// 436 -> 451 us with 0, 2 and 4 of 16 pairs for 1024 tokens behind 31744 rows) and the tensor pipe, of about the same
+// length.  So nothing may leave either idle: the batch's key tiles are cut into
 // equal shares, one per SM (paged_batch.cuh), and a CTA runs its pieces as one stream of tiles: ring, barriers and
 // tensor memory go on from piece to piece, the next piece's first logits are computed while the last one's output is
 // written.  An item that the cut divides leaves 32-bit partial outputs, which a second kernel joins in the order of the
@@ -27,10 +28,11 @@ constexpr int kTileBytes = 128 * 128 * 2;
 constexpr int kHalf = kTileBytes / 2;                    // 128 rows x 64 channels
 constexpr int kThreads = 352;                            // warp 0 loads, 1 S MMAs, 2 PV MMAs, 3..6 / 7..10 softmax
 constexpr int kSoftmaxWarps = 4;
-constexpr int kPolyPairs = 2;                            // of 16 pairs of exponentials, those on the FMA pipe
 constexpr int kEarly = 2;                                // of a tile's four groups, those before the wait for P
-constexpr int kItemUnits = 3;                            // what an item costs beside its tiles, in tiles
-constexpr int kMinUnits = 2;                             // 128-key tiles that a CTA gets at least
+// What an item costs beside its tiles, in tiles.  Ragged batch of 12 sequences, 4096 tokens alone: 0 148 / 211 us, 2
+// 119 / 176, 3 113 / 173, 4 116 / 176.
+constexpr int kItemUnits = 3;
+constexpr int kMinUnits = 4;                             // that a CTA gets at least (64 tokens behind 4096 rows: 2 25.8 us, 4 24.9)
 
 struct ChunkTail {
   uint64_t q_full, q_empty;
@@ -354,9 +356,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int j = 0; j < 32; j += 2) {
               const float2 a = ffma2(make_float2(V(g32 * 32 + j), V(g32 * 32 + j + 1)), make_float2(c2, c2),
                                      make_float2(nr, nr));
-              const int pr16 = j >> 1;
-              const bool poly = ((pr16 + 1) * kPolyPairs) / 16 > (pr16 * kPolyPairs) / 16;
-              const float2 pp = poly ? exp2_poly2(a) : make_float2(ex2_approx(a.x), ex2_approx(a.y));
+              const float2 pp = make_float2(ex2_approx(a.x), ex2_approx(a.y));
               sum2 = fadd2(sum2, pp);
               wd[j >> 1] = pack2<kF16>(pp.x, pp.y);
             }
@@ -425,8 +425,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         ok = ok && warp_wait(&tail->o_full[x], n_out & 1u, abort_flag, b.status, kDevWaitAccFull);
         ++n_out;
-        // nothing seen: the hidden logits' polynomials left 2^-125 each (a NaN stays one)
-        if (ref == -INFINITY && l < 1e-30f) l = 0.f;
         if (ok) {
           tc_fence_after();
           const int valid_tok = min(tok, walk->p.span.n - tok0);
@@ -515,65 +513,58 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   }
 }
 
-// Joins the pieces of the item that begins in share blockIdx.x and goes on behind it, if there is one: thread = query
-// row, blockIdx.y = kJoinChannels of the 128 channels.
-constexpr int kJoinChannels = 16;
-constexpr int kJoinFlight = 4;                           // contributors whose loads are in flight
+// Joins the pieces of the item that begins in share blockIdx.x and goes on behind it, if there is one: 32 of its rows
+// (lane = row), a warp per 8 channels.  Bound by latency, so the contributors' statistics are fetched side by side
+// and their outputs eight at a time.  Contributor c's slot is 1 if the item begins in its share, else 0.
+constexpr int kJoinRows = 32, kJoinThreads = 512, kJoinFlight = 8, kMaxCtas = 192;
 
 template <bool kF16>
-__global__ void __launch_bounds__(kChunkRows)
+__global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const __grid_constant__ PagedAttnParams p, int tok) {
+  __shared__ float2 ml[kMaxCtas][kJoinRows];
   grid_dep_wait();
   grid_dep_launch();
   const ChunkJoin j = p.join[blockIdx.x];
-  const int c0 = blockIdx.x, c1 = j.c_last;
-  if (c1 < 0) return;
-  const int row = threadIdx.x, x = row >> 7;
-  const int rt = (row & 127) / p.group, rh = (row & 127) - rt * p.group;
-  const int my_tok = x * tok + rt;
+  const int c0 = blockIdx.x, n = j.c_last - c0 + 1;
+  if (j.c_last < 0) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.y * kJoinRows + lane;
+  for (int c = warp; c < n; c += kJoinThreads / 32)
+    ml[c][lane] = p.chunk_ml[((c0 + c) * 2 + (c == 0)) * kChunkRows + row];
+  __syncthreads();
+  const int rt = (row & 127) / p.group, rh = (row & 127) - rt * p.group, my_tok = (row >> 7) * tok + rt;
   if (rt >= tok || my_tok >= j.n_tok) return;
-  // kJoinFlight contributors' loads in flight; contributor c0's slot is 1 (the item begins in its share), the others' 0
   float M = -INFINITY, L = 0.f;
-#pragma unroll 8
-  for (int c = c0; c <= c1; ++c) M = fmaxf(M, p.chunk_ml[(c * 2 + (c == c0)) * kChunkRows + row].x);
+  for (int c = 0; c < n; ++c) M = fmaxf(M, ml[c][lane].x);
   const float z = M == -INFINITY ? 0.f : M;
-  float4 acc[kJoinChannels / 4];
-#pragma unroll
-  for (int i = 0; i < kJoinChannels / 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = c0; c <= c1; c += kJoinFlight) {
-    float2 ml[kJoinFlight];
-    float4 v[kJoinFlight][kJoinChannels / 4];
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+  const float4* po = reinterpret_cast<const float4*>(p.chunk_o) + 2 * warp * kChunkRows + row;
+  for (int c = 0; c < n; c += kJoinFlight) {
+    float4 va[kJoinFlight], vb[kJoinFlight];
 #pragma unroll
     for (int f = 0; f < kJoinFlight; ++f) {
-      const long long slot = min(c + f, c1) * 2 + (c + f == c0);
-      ml[f] = p.chunk_ml[slot * kChunkRows + row];
-      const float4* po = reinterpret_cast<const float4*>(p.chunk_o) + slot * (kChunkRows * 32) +
-                         blockIdx.y * (kJoinChannels / 4) * kChunkRows + row;
-#pragma unroll
-      for (int i = 0; i < kJoinChannels / 4; ++i) v[f][i] = po[i * kChunkRows];
+      const int cc = min(c + f, n - 1);
+      const float4* at = po + static_cast<long long>((c0 + cc) * 2 + (cc == 0)) * (kChunkRows * 32);
+      va[f] = at[0];
+      vb[f] = at[kChunkRows];
     }
 #pragma unroll
     for (int f = 0; f < kJoinFlight; ++f) {
-      const float s = ex2_approx(ml[f].x - z);
-      if (c + f <= c1 && (s != 0.f || isnan(ml[f].y))) {         // where the row saw nothing, O may hold anything
-        L = fmaf(ml[f].y, s, L);
-#pragma unroll
-        for (int i = 0; i < kJoinChannels / 4; ++i) {
-          acc[i].x = fmaf(v[f][i].x, s, acc[i].x); acc[i].y = fmaf(v[f][i].y, s, acc[i].y);
-          acc[i].z = fmaf(v[f][i].z, s, acc[i].z); acc[i].w = fmaf(v[f][i].w, s, acc[i].w);
-        }
+      if (c + f >= n) break;
+      const float2 x = ml[c + f][lane];
+      const float s = ex2_approx(x.x - z);
+      if (s != 0.f || isnan(x.y)) {                      // where the row saw nothing, O may hold anything
+        L = fmaf(x.y, s, L);
+        a.x = fmaf(va[f].x, s, a.x); a.y = fmaf(va[f].y, s, a.y); a.z = fmaf(va[f].z, s, a.z); a.w = fmaf(va[f].w, s, a.w);
+        b.x = fmaf(vb[f].x, s, b.x); b.y = fmaf(vb[f].y, s, b.y); b.z = fmaf(vb[f].z, s, b.z); b.w = fmaf(vb[f].w, s, b.w);
       }
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const long long at = (static_cast<long long>(j.token) + my_tok) * p.n_q + j.head * p.group + rh;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * 128 + blockIdx.y * kJoinChannels);
-#pragma unroll
-  for (int i = 0; i < kJoinChannels / 4; i += 2)
-    *reinterpret_cast<uint4*>(dst + 2 * i) =
-        make_uint4(pack2<kF16>(acc[i].x * inv, acc[i].y * inv), pack2<kF16>(acc[i].z * inv, acc[i].w * inv),
-                   pack2<kF16>(acc[i + 1].x * inv, acc[i + 1].y * inv), pack2<kF16>(acc[i + 1].z * inv, acc[i + 1].w * inv));
-  if (p.lse && blockIdx.y == 0) p.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718f;
+  reinterpret_cast<uint4*>(p.out)[at * 16 + warp] =
+      make_uint4(pack2<kF16>(a.x * inv, a.y * inv), pack2<kF16>(a.z * inv, a.w * inv), pack2<kF16>(b.x * inv, b.y * inv),
+                 pack2<kF16>(b.z * inv, b.w * inv));
+  if (p.lse && warp == 0) p.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718f;
 }
 
 }  // namespace
@@ -587,11 +578,12 @@ cudaError_t init_paged_chunk() {
 cudaError_t launch_paged_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                const PagedAttnParams& p, bool f16, int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
+  if (n_sm > kMaxCtas) return cudaErrorInvalidConfiguration;
   const TileShape ts = {p.n_kv, 2 * (128 / p.group), 7, kItemUnits};
   const cudaError_t e = launch_after_previous(k, n_sm, kThreads, kSmem, st, map_q, map_k, map_v, p, ts);
   if (e != cudaSuccess) return e;
   auto j = f16 ? paged_join_kernel<true> : paged_join_kernel<false>;
-  return launch_after_previous(j, dim3(n_sm, 128 / kJoinChannels), kChunkRows, 0, st, p, 128 / p.group);
+  return launch_after_previous(j, dim3(n_sm, kChunkRows / kJoinRows), kJoinThreads, 0, st, p, 128 / p.group);
 }
 
 }  // namespace ilre
