@@ -260,7 +260,7 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out) {
   ok = ok && dev_alloc(h, &h->chunk_o, static_cast<size_t>(h->n_sm) * 2 * kChunkRows * kDim);
   ok = ok && dev_alloc(h, &h->chunk_ml, static_cast<size_t>(h->n_sm) * 2 * kChunkRows);
   ok = ok && dev_alloc(h, &h->join, h->n_sm);
-  ok = ok && dev_alloc(h, &h->w_part, static_cast<size_t>(h->n_sm) * 2 * 128);
+  ok = ok && dev_alloc(h, &h->w_part, static_cast<size_t>(h->n_sm) * 2 * 256);
   ok = ok && dev_alloc(h, &h->n_keep, cfg->max_seqs);
   ok = ok && dev_alloc(h, &h->status, 1);
   if (ok) ok = cudaMemset(h->status, 0, sizeof(int)) == cudaSuccess;

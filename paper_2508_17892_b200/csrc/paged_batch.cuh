@@ -66,7 +66,7 @@ struct HeadTiles {
 // the tiles of `tq` query tokens that see any of them.  (The names are HeadTiles': "query tile" is the item's
 // number, "key tiles" are its units.)
 struct KeyTiles {
-  int n, kv, tq, tk_shift, extra;          // extra: 0
+  int n, kv, tq, tk_shift, extra;
   __host__ __device__ int n_qt() const { return static_cast<int>((static_cast<unsigned>(kv) + (1u << tk_shift) - 1) >> tk_shift); }
   __host__ __device__ int row_tiles() const { return n <= tq ? 1 : static_cast<int>(static_cast<unsigned>(n + tq - 1) / tq); }
   // the first row tile that sees a key of tile kt
@@ -80,12 +80,14 @@ struct KeyTiles {
   __host__ __device__ long long before(int kt) const {
     const int pre = kv - n;
     const int seen = pre <= 0 ? 0 : static_cast<int>((static_cast<unsigned>(pre) + (1u << tk_shift) - 1) >> tk_shift);
-    const long long all = static_cast<long long>(kt) * row_tiles();
+    const long long all = static_cast<long long>(kt) * (row_tiles() + extra);
     if (seen >= kt) return all;
     const unsigned b = static_cast<unsigned>((seen << tk_shift) - pre);
     int z = 0;
     while (z < tk_shift && !((tq >> z) & 1)) ++z;
     const int P = tq >> z, s = 1 << (tk_shift - z), terms = kt - seen;
+    if (P == 1)                            // tq a power of two: first(i) = (b >> z) + i s
+      return all - (static_cast<long long>(terms) * (b >> z) + static_cast<long long>(s) * terms * (terms - 1) / 2);
     const long long k = terms / P;
     const int r = terms - static_cast<int>(k) * P;
     long long whole = 0, rest = 0;
@@ -99,7 +101,7 @@ struct KeyTiles {
   __host__ __device__ long long units() const {
     if (n <= 0 || kv <= 0) return 0;
     const int last = n_qt() - 1;
-    return before(last) + key_tiles(last);
+    return before(last) + key_tiles(last) + extra;
   }
   __host__ __device__ int tile_of(long long u) const {
     int lo = 0, hi = n_qt() - 1;
@@ -200,38 +202,44 @@ struct Item {
   __host__ __device__ long long end(const TileShape& ts) const { return begin + ts.extra + n_tiles; }
 };
 
-// The query tile of a head's unit.  On the device all lanes of a warp ask together and try 32 tiles at a time.
+// The query tile of a head's unit, and the units before it.  On the device all lanes of a warp ask together and try 32
+// tiles at a time.
 template <class Tiles>
-__host__ __device__ __forceinline__ int find_tile(const Tiles& t, long long u) {
+__host__ __device__ __forceinline__ int find_tile(const Tiles& t, long long u, long long* before) {
 #ifdef __CUDA_ARCH__
   const int lane = threadIdx.x & 31;
   int lo = 0, n = t.n_qt();                // in [lo, lo + n)
+  *before = 0;
   while (n > 1) {
     const int step = (n + 31) >> 5, qt = lo + lane * step;
-    const bool at_or_behind = lane * step < n && t.before(qt) <= u;
-    const int k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, at_or_behind));              // lane 0's is true
+    const long long mine = lane * step < n ? t.before(qt) : 0;
+    const int k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, lane * step < n && mine <= u));      // lane 0's is true
+    *before = __shfl_sync(0xFFFFFFFFu, mine, k);
     n = min(step, n - k * step);
     lo += k * step;
   }
   return lo;
 #else
-  return t.tile_of(u);
+  const int qt = t.tile_of(u);
+  *before = t.before(qt);
+  return qt;
 #endif
 }
 
-// The item of unit `at` of the sequence `seq` whose first unit is seq_begin.
+// The item of unit `at` of the sequence `seq` of `units` units, the first of which is seq_begin.
 template <class Tiles>
-__host__ __device__ __forceinline__ Item locate(const PagedBatch& b, const TileShape& ts, int seq, long long seq_begin,
-                                                long long at) {
+__host__ __device__ __forceinline__ Item locate(const TileShape& ts, int seq, const SeqSpan& span, long long units,
+                                                long long seq_begin, long long at) {
   Item x;
   x.seq = seq;
-  x.span = load_span(b, seq);
-  const Tiles tiles{x.span.n, x.span.kv, ts.tq, ts.tk_shift, ts.extra};
-  const long long per_head = tiles.units(), off = at - seq_begin;
+  x.span = span;
+  const Tiles tiles{span.n, span.kv, ts.tq, ts.tk_shift, ts.extra};
+  const long long per_head = div_pos(units, ts.heads), off = at - seq_begin;
   x.head = static_cast<int>(div_pos(off, per_head));
   const long long in_head = off - x.head * per_head;
-  x.qt = find_tile(tiles, in_head);
-  x.begin = at - in_head + tiles.before(x.qt);
+  long long before;
+  x.qt = find_tile(tiles, in_head, &before);
+  x.begin = at - in_head + before;
   x.n_tiles = tiles.key_tiles(x.qt);
   return x;
 }

@@ -52,7 +52,8 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
     if (base >= u1) break;
   }
   if (warp < 2) {
-    const Item x = locate<Tiles>(b, ts, static_cast<int>(found[2 * warp]), found[2 * warp + 1], warp ? u1 - 1 : u0);
+    const int seq = static_cast<int>(found[2 * warp]);
+    const Item x = locate<Tiles>(ts, seq, load_span(b, seq), seq_units<Tiles>(b, ts, seq), found[2 * warp + 1], warp ? u1 - 1 : u0);
     if (lane == 0) { if (warp) out->last = x; else out->first = x; }
   }
 }
@@ -62,13 +63,18 @@ template <class Tiles>
 __device__ __forceinline__ void plan_small(const PagedBatch& b, const TileShape& ts, int min_units, PlanStart* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (warp >= 2) return;
-  const long long n = lane < b.n_seqs ? seq_units<Tiles>(b, ts, lane) : 0;
+  SeqSpan span = {0, 0, 0};
+  long long n = 0;
+  if (lane < b.n_seqs) {
+    span = load_span(b, lane);
+    if (in_range(b, span.n)) n = Tiles{span.n, span.kv, ts.tq, ts.tk_shift, ts.extra}.units() * ts.heads;
+  }
   long long incl = n;
-  for (int o = 1; o < 32; o <<= 1) {
+  for (int o = 1; o < 32 && o < b.n_seqs; o <<= 1) {
     const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
     if (lane >= o) incl += v;
   }
-  const long long total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+  const long long total = __shfl_sync(0xFFFFFFFFu, incl, b.n_seqs - 1);
   const int n_cta = share_ctas(total, gridDim.x, min_units), c = blockIdx.x;
   const bool has = total > 0 && c < n_cta;
   const long long u0 = has ? share_begin(total, n_cta, c) : 0, u1 = has ? share_begin(total, n_cta, c + 1) : 0;
@@ -76,7 +82,8 @@ __device__ __forceinline__ void plan_small(const PagedBatch& b, const TileShape&
   if (!has) return;
   const long long at = warp ? u1 - 1 : u0, begin = incl - n;
   const int seq = __ffs(__ballot_sync(0xFFFFFFFFu, begin <= at && at < incl)) - 1;
-  const Item x = locate<Tiles>(b, ts, seq, __shfl_sync(0xFFFFFFFFu, begin, seq), at);
+  span = SeqSpan{__shfl_sync(0xFFFFFFFFu, span.q0, seq), __shfl_sync(0xFFFFFFFFu, span.n, seq), __shfl_sync(0xFFFFFFFFu, span.kv, seq)};
+  const Item x = locate<Tiles>(ts, seq, span, __shfl_sync(0xFFFFFFFFu, n, seq), __shfl_sync(0xFFFFFFFFu, begin, seq), at);
   if (lane == 0) { if (warp) out->last = x; else out->first = x; }
 }
 

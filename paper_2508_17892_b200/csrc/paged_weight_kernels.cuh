@@ -17,8 +17,8 @@ struct PagedWeightParams {
   float* w;                                      // [n_pages][n_kv][page_size]
   int n_q, n_kv, group;
   float c2;
-  float* part;                                   // [CTA][2][128]: sums of the pieces of cut items
-  uint32_t* arrived;                             // [CTA], 0 between launches
+  float* part;                                   // [CTA][2][256]: sums of the pieces of cut items
+  uint32_t* arrived;                             // [CTA][2], 0 between launches
 };
 
 struct EvictParams {
@@ -40,7 +40,7 @@ cudaError_t init_paged_weights();
 cudaError_t init_paged_weight_rows();
 cudaError_t init_evict();
 
-// Query tokens of a row tile: 128 rows, or all that any sequence has.
+// Query tokens of a row tile: up to 64 rows (one token of a larger group), or all that any sequence has.
 int weight_tile_tokens(int group, int max_q_len);
 // map_q: {channel, head, token}, boxes of 64 channels x group x weight_tile_tokens; map_k: the pool as {channel, kv head,
 // row, page}, boxes of 64 channels x min(page_size, 128) rows.

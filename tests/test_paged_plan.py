@@ -21,12 +21,10 @@ static int bad = 0;
 const int tqs[] = {1, 2, 4, 16, 50, 64, 256}, tks[] = {6, 7};
 struct Q : HeadTiles {
   Q(int n, int kv, int tq, int tk, int extra) : HeadTiles{n, kv, tq, tk, extra} {}
-  static constexpr bool kExtra = true;
   static bool counts(int) { return true; }
 };
 struct K : KeyTiles {
   K(int n, int kv, int tq, int tk, int extra) : KeyTiles{n, kv, tq, tk, extra} {}
-  static constexpr bool kExtra = false;
   static bool counts(int kv) { return kv > 0; }
 };
 
@@ -48,7 +46,7 @@ void batches(std::mt19937& rng) {
     int status = 0;
     PagedBatch b{n, pick(0, 5) ? q_start[n] : q_start[n] + 3, max_q, max_blocks, page_shift, 1, 0, 1 << 30, q_start.data(), kv.data(),
                  table.data(), &status};
-    const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2], Tiles::kExtra ? pick(0, 3) : 0};
+    const TileShape ts{pick(1, 5), tqs[rng() % 7], tks[rng() % 2], pick(0, 3)};
     std::vector<long long> units(n), begin(n + 1, 0);
     for (int i = 0; i < n; ++i) {
       const long long len = static_cast<long long>(q_start[i + 1]) - q_start[i];
@@ -74,8 +72,8 @@ void batches(std::mt19937& rng) {
       int a = 0, z = 0;
       while (begin[a + 1] <= s.u0) ++a;
       while (begin[z + 1] < s.u1) ++z;
-      s.first = locate<Tiles>(b, ts, a, begin[a], s.u0);
-      s.last = locate<Tiles>(b, ts, z, begin[z], s.u1 - 1);
+      s.first = locate<Tiles>(ts, a, load_span(b, a), units[a], begin[a], s.u0);
+      s.last = locate<Tiles>(ts, z, load_span(b, z), units[z], begin[z], s.u1 - 1);
       PieceWalk<Tiles> w;
       std::vector<Piece> pieces;            // the last one comes first
       for (bool more = w.begin(b, ts, s); more; more = w.next(b, ts, s)) pieces.push_back(w.p);
@@ -129,7 +127,7 @@ int main() {
   // the same from the keys: the row tiles that see a key of the tile
   const int tts[] = {1, 2, 3, 18, 25, 32, 42, 128};
   for (int i = 0; i < 4000; ++i) {
-    KeyTiles h{pick(1, 400), pick(1, 3) > 1 ? pick(1, 2000) : pick(1, 5), tts[rng() % 8], 7, 0};
+    KeyTiles h{pick(1, 400), pick(1, 3) > 1 ? pick(1, 2000) : pick(1, 5), tts[rng() % 8], 7, pick(0, 1) * 3};
     long long at = 0;
     for (int kt = 0; kt < h.n_qt(); ++kt) {
       int seen = 0;
@@ -139,8 +137,8 @@ int main() {
       }
       CHECK(seen >= 1 && h.key_tiles(kt) == seen && h.first(kt) == h.row_tiles() - seen);
       CHECK(h.before(kt) == at);
-      for (long long u = at; u < at + seen; u += 3) CHECK(h.tile_of(u) == kt);
-      at += seen;
+      for (long long u = at; u < at + seen + h.extra; u += 3) CHECK(h.tile_of(u) == kt);
+      at += seen + h.extra;
     }
     CHECK(h.units() == at);
   }
@@ -148,7 +146,7 @@ int main() {
   HeadTiles far{1 << 30, 2147481000, 64, 7, 3};
   CHECK(far.units() > 0 && far.before(far.n_qt() - 1) < far.units());
   CHECK(far.tile_of(far.units() - 1) == far.n_qt() - 1);
-  KeyTiles far_k{1 << 30, 2147481000, 18, 7, 0};
+  KeyTiles far_k{1 << 30, 2147481000, 18, 7, 3};
   CHECK(far_k.tile_of(far_k.units() - 1) == far_k.n_qt() - 1 && far_k.key_tiles(far_k.n_qt() - 1) >= 1);
 
   batches<Q>(rng);
