@@ -421,7 +421,7 @@ int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride,
  * ilre_recall_run, [page_size][n_kv_heads][128], so a cache [L][n_kv_heads][128] is a pool of
  * L / page_size pages.
  *
- * The handle owns the workspace of the split work (about 60 MB) and nothing of the cache.  It may be
+ * The handle owns the workspace of the split work (about 45 MB) and nothing of the cache.  It may be
  * used from one host thread and one stream at a time; calls captured into graphs use its workspace
  * too, so graphs of one handle must not run at the same time as each other or as other calls of it.
  */
@@ -518,7 +518,7 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
  * weights become rows 0, 1, ... in their old order: in the sequence's own pages (dst_table_dev NULL; their
  * pages must then be on one place of one sequence's table only), or in the pages of dst_table_dev
  * [n_seqs][dst_blocks] (dst_blocks * page_size >= budget; disjoint from the pages of the batch).  Weights are >= 0
- * (others rank by the order of their bits, NaN included).
+ * (NaN counts as the largest, zeros of either sign as equal; lower ones rank below).
  *   kept_out_dev     int32 [n_seqs][per_head ? n_kv_heads : 1][budget]: kept rows ascending, then -1
  *   new_len_out_dev  int32 [n_seqs]: min(kv_len, budget); may be kv_len_dev itself
  * q_start_dev is not read (may be NULL).  n_sink + n_recent <= budget (ILRE_ERR_BUDGET).

@@ -182,7 +182,7 @@ struct KernelChoice {
 KernelChoice choose_kernels(const ilre_paged_batch_t& b, int group) {
   KernelChoice c;
   c.row_tokens = kRowTile / group;
-  c.chunks = b.max_q_len > c.row_tokens;
+  c.chunks = b.max_q_len > c.row_tokens || c.row_tokens == 0;
   c.rows = c.row_tokens > 0 && (!c.chunks || b.n_seqs > 1);
   return c;
 }

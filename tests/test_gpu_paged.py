@@ -569,3 +569,89 @@ def test_other_stream_and_captured_graph():
         for x, y in zip(replayed, (out, lse, t["k_pool"], t["w_pool"], kept, new_len)):
             assert torch.equal(x, y)
     _close(eng)
+
+
+# ---- sizes that cross the kernels' own bounds ------------------------------------------------------
+
+@pytest.mark.parametrize("group", [1, 2, 3, 6, 11, 15, 16, 17, 31, 48, 64, 65, 100, 128])
+def test_every_size_of_a_group(group):
+    """Query heads per kv head: those that share a tile of 16, 64 or 128 rows, fill it or leave rows of it over."""
+    for n_new in (1, 2, 9):
+        b = ref.Batch([n_new, 1], [n_new + 150, 131], 16, 1 if group > 16 else 2, group * (1 if group > 16 else 2),
+                      seed=group * 10 + n_new).poison()
+        eng = _engine(b)
+        t = b.gpu(eng)
+        out, lse = eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], want_lse=True)
+        want, want_lse, tol, tol_lse = ref.attention(b)
+        assert bool(((out.double().cpu() - want).abs() <= tol).all())
+        assert bool(((lse.double().cpu() - want_lse).abs() <= tol_lse).all())
+        w = t["w_pool"].clone()
+        eng.accumulate(t["batch"], t["q"], lse, t["k_pool"], w)
+        want_w, tol_w = ref.accumulate(b, lse.cpu())
+        assert bool(((w.double().cpu() - want_w).abs() <= tol_w).all())
+        _close(eng)
+
+
+@pytest.mark.parametrize("n_new", [1, 4, 5, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129])
+def test_lengths_around_the_tiles(n_new):
+    """New tokens and rows on both sides of the tiles' 16, 64, 128 and 256."""
+    kv = [n_new, max(n_new, 63), n_new + 64, n_new + 65, max(n_new, 128), n_new + 127, n_new + 256]
+    b = ref.Batch([n_new] * len(kv), kv, 32, 1, 4, seed=n_new, dtype=FP if n_new % 2 else BF).poison()
+    eng = _engine(b)
+    t = b.gpu(eng)
+    out, lse = eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], want_lse=True)
+    want, want_lse, tol, tol_lse = ref.attention(b)
+    assert bool(((out.double().cpu() - want).abs() <= tol).all())
+    assert bool(((lse.double().cpu() - want_lse).abs() <= tol_lse).all())
+    w = t["w_pool"].clone()
+    eng.accumulate(t["batch"], t["q"], lse, t["k_pool"], w)
+    want_w, tol_w = ref.accumulate(b, lse.cpu())
+    assert bool(((w.double().cpu() - want_w).abs() <= tol_w).all())
+    _close(eng)
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pools of more than 2^31 elements: the sequences' pages are the first and the last ones."""
+    from paper_2508_17892_b200 import PagedCache
+    n_kv, n_q, page = 8, 16, 128
+    n_pages = (1 << 31) // (page * n_kv * 128) + 40
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k_pool, v_pool = (torch.zeros(n_pages, page, n_kv, 128, dtype=BF, device="cuda") for _ in range(2))
+    assert k_pool.numel() > 1 << 31
+    w_pool = torch.zeros(n_pages, n_kv, page, device="cuda")
+    b = ref.Batch([3, 40], [600, 300], page, n_kv, n_q, seed=4, spare=5, garbage=False)
+    far = torch.tensor([0, 1] + list(range(n_pages - b.n_pages + 2, n_pages)))     # page i of the small pool lies here
+    k_pool[far], v_pool[far], w_pool[far] = b.k_pool.cuda(), b.v_pool.cuda(), b.w_pool.cuda()
+    eng = PagedCache(n_kv_heads=n_kv, n_q_heads=n_q, page_size=page, max_seqs=2)
+    small = b.gpu(eng)
+    table = far[b.table.long()].to(torch.int32).cuda()
+    batch = eng.batch(small["q_start"], small["kv_len"], table, b.n_tokens, b.max_q)
+    spec = _spec()
+    q = eng.append(batch, small["q"], small["k"], small["v"], small["pos"], spec, k_pool, v_pool, w_pool)
+    q2 = eng.append(small["batch"], small["q"], small["k"], small["v"], small["pos"], spec, small["k_pool"], small["v_pool"],
+                    small["w_pool"])
+    out, lse = eng.attention(batch, q, k_pool, v_pool, want_lse=True)
+    out2, lse2 = eng.attention(small["batch"], q2, small["k_pool"], small["v_pool"], want_lse=True)
+    eng.accumulate(batch, q, lse, k_pool, w_pool)
+    eng.accumulate(small["batch"], q2, lse2, small["k_pool"], small["w_pool"])
+    kept, _ = eng.evict(batch, 200, 2, 30, k_pool, v_pool, w_pool)
+    kept2, _ = eng.evict(small["batch"], 200, 2, 30, small["k_pool"], small["v_pool"], small["w_pool"])
+    for x, y in ((q, q2), (out, out2), (lse, lse2), (kept, kept2), (k_pool[far], small["k_pool"]),
+                 (v_pool[far], small["v_pool"]), (w_pool[far], small["w_pool"])):
+        assert torch.equal(x, y)
+    want, _, tol, _ = ref.attention(_as_now(b, small, q2, out2))
+    assert bool(((out.double().cpu() - want).abs() <= tol).all())
+    _close(eng)
+
+
+def _as_now(b, small, q, out):
+    """The batch with its rows as `append` left them (before the eviction moved them, which this undoes by appending
+    to a fresh copy)."""
+    from paper_2508_17892_b200 import PagedCache
+    fresh = ref.Batch(b.q_len, b.kv_len_list, b.page, b.n_kv, b.n_q, seed=4, spare=5, garbage=False)
+    eng = PagedCache(n_kv_heads=b.n_kv, n_q_heads=b.n_q, page_size=b.page, max_seqs=2)
+    t = fresh.gpu(eng)
+    fresh.q = eng.append(t["batch"], t["q"], t["k"], t["v"], t["pos"], _spec(), t["k_pool"], t["v_pool"]).cpu()
+    fresh.k_pool, fresh.v_pool = t["k_pool"].cpu(), t["v_pool"].cpu()
+    eng.close()
+    return fresh
