@@ -97,12 +97,17 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr() if t is not None else None
 
 
-def _rows(t: torch.Tensor, device, dtype, heads: int, dim: int) -> int:
+def _rows(t: torch.Tensor, index: int, dtype, heads: int, dim: int) -> int:
     """Stride in elements from token to token of a tensor [n, heads, dim] whose tokens are contiguous."""
-    assert t.device == device and t.dtype == dtype and t.dim() == 3
-    (n, h, d), (st, sh, sd) = t.shape, t.stride()
-    assert h == heads and d == dim and (n == 0 or (sd == 1 and (heads == 1 or sh == dim)))
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    assert h == heads and d == dim and t.dtype == dtype and t.get_device() == index
+    assert n == 0 or (sd == 1 and (heads == 1 or sh == dim))
     return st if n > 1 else heads * dim
+
+
+def _ints(t: torch.Tensor, index: int, n: int) -> None:
+    assert t.get_device() == index and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous()
 
 
 class _OnStream:
@@ -135,19 +140,19 @@ def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: b
 
     ``out`` may be ``x``.  ``transposed`` applies the transposed map: the gradient of ``rope`` with
     respect to x is ``rope(grad, positions, spec, transposed=True)``."""
-    assert x.is_cuda and x.dtype in _DTYPES and x.dim() == 3
+    dtype, index = x.dtype, x.get_device()
+    assert index >= 0 and dtype in _DTYPES
     n, heads, dim = x.shape
-    assert positions.device == x.device and positions.dtype == torch.int32 and positions.is_contiguous()
-    assert positions.shape == (n,)
-    x_stride = _rows(x, x.device, x.dtype, heads, dim)
+    _ints(positions, index, n)
+    x_stride = _rows(x, index, dtype, heads, dim)
     with _OnStream(x.device, stream, (x, positions, out)) as st:
         if out is None:
-            out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
-        out_stride = _rows(out, x.device, x.dtype, heads, dim)
+            out = torch.empty(n, heads, dim, dtype=dtype, device=x.device)
+        out_stride = _rows(out, index, dtype, heads, dim)
         assert out.shape[0] == n
         args = (spec.ref, x.data_ptr(), x_stride, out.data_ptr(), out_stride, positions.data_ptr(), n, heads, dim,
-                _DTYPES[x.dtype], int(transposed), st)
-        if torch.cuda.current_device() == x.device.index:
+                _DTYPES[dtype], int(transposed), st)
+        if torch.cuda.current_device() == index:
             rc = load_library().ilre_rope(*args)
         else:
             with torch.cuda.device(x.device):
@@ -175,7 +180,9 @@ class PagedCache:
             raise IlreError(rc, "ilre_paged_create")
         self.dtype, self._n_q, self._dim = dtype, n_q_heads, head_dim
         self.device = torch.device("cuda", device)
+        self._index = device
         self._page_shape = (page_size, n_kv_heads, head_dim)
+        self._weight_shape = (n_kv_heads, page_size)
         self._page_stride = (n_kv_heads * head_dim, head_dim, 1)
 
     def batch(self, q_start: Optional[torch.Tensor], kv_len: torch.Tensor, block_table: torch.Tensor, n_tokens: int,
@@ -188,25 +195,26 @@ class PagedCache:
         assert q_start is None or q_start.shape == (kv_len.numel() + 1,)
         return PagedBatch(q_start, kv_len, block_table, n_tokens, max_q_len)
 
+    def _page_step(self, t: Optional[torch.Tensor], shape) -> int:
+        """Stride in elements from page to page (0: back to back)."""
+        if t is None:
+            return 0
+        assert t.shape == shape and t.dtype == self.dtype and t.get_device() == self._index
+        step = t.stride()
+        assert step[1:] == self._page_stride or shape[0] == 0 or t[0].is_contiguous()
+        return step[0] if shape[0] > 1 else 0
+
     def _pool(self, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
-        c, n_pages = self.cfg, k.shape[0]
-        page = self._page_shape
-
-        def stride(t):
-            if t is None:
-                return 0
-            assert t.device == self.device and t.dtype == self.dtype and t.shape == (n_pages,) + page
-            first, rest = t.stride()[0], t.stride()[1:]
-            assert n_pages == 0 or rest == self._page_stride or t[0].is_contiguous()
-            return first if n_pages > 1 else 0
-
-        assert w is None or (w.device == self.device and w.dtype == torch.float32 and w.is_contiguous() and
-                             w.shape == (n_pages, c.n_kv_heads, c.page_size))
-        return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), stride(k), stride(v), n_pages)
+        n_pages = k.shape[0]
+        shape = (n_pages,) + self._page_shape
+        assert w is None or (w.shape == (n_pages,) + self._weight_shape and w.dtype == torch.float32 and
+                             w.is_contiguous() and w.get_device() == self._index)
+        return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), self._page_step(k, shape), self._page_step(v, shape), n_pages)
 
     def _q(self, batch: PagedBatch, q: torch.Tensor) -> int:
-        assert q.shape[0] == batch.n_tokens and (batch.n_tokens == 0 or batch.q_start is not None)
-        return _rows(q, self.device, self.dtype, self._n_q, self._dim)
+        n = batch.n_tokens
+        assert q.shape[0] == n and (n == 0 or batch.q_start is not None)
+        return _rows(q, self._index, self.dtype, self._n_q, self._dim)
 
     def _check(self, rc: int, what: str) -> None:
         if rc != 0:
@@ -218,15 +226,13 @@ class PagedCache:
                stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
         """k turned and v copied to the new tokens' rows, their weights cleared; returns q turned (``q_out``, which
         may be q; made here if not given).  spec None: nothing is turned."""
-        c = self.cfg
-        n = batch.n_tokens
+        n, n_kv, dim = batch.n_tokens, self._page_shape[1], self._dim
         assert k.shape[0] == n and v.shape[0] == n
-        k_stride, v_stride = (_rows(t, self.device, self.dtype, c.n_kv_heads, c.head_dim) for t in (k, v))
-        if spec is not None:
-            assert positions is not None
+        k_stride = _rows(k, self._index, self.dtype, n_kv, dim)
+        v_stride = _rows(v, self._index, self.dtype, n_kv, dim)
+        assert spec is None or positions is not None
         if positions is not None:
-            assert positions.device == self.device and positions.dtype == torch.int32 and positions.is_contiguous()
-            assert positions.shape == (n,)
+            _ints(positions, self._index, n)
         pool = self._pool(k_pool, v_pool, w_pool)
         with _OnStream(self.device, stream, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start,
                                              batch.kv_len, batch.block_table)) as st:
@@ -234,7 +240,7 @@ class PagedCache:
             if q is not None:
                 q_stride = self._q(batch, q)
                 if q_out is None:
-                    q_out = torch.empty(n, c.n_q_heads, c.head_dim, dtype=q.dtype, device=q.device)
+                    q_out = torch.empty(n, self._n_q, dim, dtype=q.dtype, device=q.device)
                 q_out_stride = self._q(batch, q_out)
             else:
                 assert q_out is None
@@ -249,17 +255,17 @@ class PagedCache:
                   stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """Every new token over its sequence's cached rows up to itself: (out like q, lse fp32 [n_tokens, n_q_heads]
         or None).  Rows of tokens that belong to no sequence are left as they are."""
-        c = self.cfg
         q_stride = self._q(batch, q)
         pool = self._pool(k_pool, v_pool, None)
+        shape = (batch.n_tokens, self._n_q, self._dim)
         with _OnStream(self.device, stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len,
                                              batch.block_table)) as st:
             if out is None:
-                out = torch.empty(batch.n_tokens, c.n_q_heads, c.head_dim, dtype=q.dtype, device=q.device)
+                out = torch.empty(shape, dtype=q.dtype, device=q.device)
             if lse is None and want_lse:
-                lse = torch.empty(batch.n_tokens, c.n_q_heads, dtype=torch.float32, device=q.device)
-            assert out.device == self.device and out.dtype == self.dtype and out.is_contiguous()
-            assert out.shape == (batch.n_tokens, c.n_q_heads, c.head_dim)
+                lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+            assert out.shape == shape and out.dtype == self.dtype and out.is_contiguous()
+            assert out.get_device() == self._index
             self._lse(batch, lse)
             self._check(self._lib.ilre_paged_attention(
                 self._h, batch.ref, q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
@@ -267,8 +273,8 @@ class PagedCache:
         return out, lse
 
     def _lse(self, batch: PagedBatch, lse: Optional[torch.Tensor]) -> None:
-        assert lse is None or (lse.device == self.device and lse.dtype == torch.float32 and lse.is_contiguous() and
-                               lse.shape == (batch.n_tokens, self.cfg.n_q_heads))
+        assert lse is None or (lse.shape == (batch.n_tokens, self._n_q) and lse.dtype == torch.float32 and
+                               lse.is_contiguous() and lse.get_device() == self._index)
 
     def accumulate(self, batch: PagedBatch, q: torch.Tensor, lse: torch.Tensor, k_pool: torch.Tensor,
                    w_pool: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
@@ -294,7 +300,7 @@ class PagedCache:
         int32 [n_seqs, n_kv_heads or 1, budget], ascending, -1 behind a shorter sequence; new_len int32 [n_seqs],
         which may be batch.kv_len)."""
         n = batch.kv_len.numel()
-        shape = (n, self.cfg.n_kv_heads if per_head else 1, budget)
+        shape = (n, self._page_shape[1] if per_head else 1, budget)
         assert budget >= 1 and w_pool is not None
         pool = self._pool(k_pool, v_pool, w_pool)
         if dst_table is not None:
@@ -307,7 +313,7 @@ class PagedCache:
             if new_len is None:
                 new_len = torch.empty(n, dtype=torch.int32, device=self.device)
             for t, want in ((kept, shape), (new_len, (n,))):
-                assert t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and t.shape == want
+                assert t.shape == want and t.dtype == torch.int32 and t.is_contiguous() and t.get_device() == self._index
             self._check(self._lib.ilre_paged_evict(
                 self._h, batch.ref, budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
                 _ptr(dst_table), dst_table.shape[1] if dst_table is not None else 0, kept.data_ptr(),
