@@ -35,6 +35,7 @@ enum ilre_status {
   ILRE_ERR_CAPACITY = -3,     /* L, q_len, budget or #combinations above the create() caps  */
   ILRE_ERR_BUDGET = -4,       /* budget > L - n_sink                                         */
   ILRE_ERR_ALIGNMENT = -5,    /* key cache or query base address not 16-byte aligned         */
+                              /* (int32 and fp32 arrays of the paged cache: 4-byte)          */
   ILRE_ERR_CUDA = -6,         /* a CUDA runtime/driver call failed                           */
   ILRE_ERR_DEVICE_WAIT = -7,  /* a bounded wait inside a kernel gave up (see _status)        */
   ILRE_ERR_QUOTA = -8,        /* a combination ran out of candidates (cannot happen for valid */

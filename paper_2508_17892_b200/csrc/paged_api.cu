@@ -42,6 +42,7 @@ constexpr int kDim = 128;
 constexpr double kPi = 3.14159265358979323846;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }    // int32 and fp32 arrays; null passes
 
 void free_all(ilre_paged* h) {
   cudaFree(h->part_o); cudaFree(h->part_ml); cudaFree(h->arrived); cudaFree(h->n_keep); cudaFree(h->chunk_o);
@@ -120,6 +121,8 @@ int validate_batch(const ilre_paged* h, const ilre_paged_batch_t* b, const ilre_
   if (b->n_seqs > h->cfg.max_seqs ||
       static_cast<long long>(b->max_blocks) * h->cfg.page_size >= 2147483647LL - 2048)
     return ILRE_ERR_CAPACITY;
+  if (!aligned4(b->q_start_dev) || !aligned4(b->kv_len_dev) || !aligned4(b->block_table_dev) || !aligned4(pool->w_dev))
+    return ILRE_ERR_ALIGNMENT;
   int shift = 0;
   while ((1 << shift) < h->cfg.page_size) ++shift;
   *out = PagedBatch{b->n_seqs, b->n_tokens, b->max_q_len, b->max_blocks, shift, pool->n_pages, 0, 2147483647, b->q_start_dev,
@@ -209,6 +212,7 @@ int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride,
   ILRE_CHECK(make_freqs(spec, head_dim, &f));
   if (n_tokens == 0) return ILRE_OK;
   if (!pos_dev) return ILRE_ERR_INVALID_ARG;
+  if (!aligned4(pos_dev)) return ILRE_ERR_ALIGNMENT;
   ILRE_CHECK(validate_rows(x_dev, x_stride, n_heads, head_dim));
   ILRE_CHECK(validate_rows(out_dev, out_stride, n_heads, head_dim));
   int dev = 0, n_sm = 0;
@@ -288,6 +292,7 @@ int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const il
   ILRE_CHECK(make_freqs(spec, kDim, &f));
   if (batch->n_tokens == 0 || batch->n_seqs == 0) return ILRE_OK;
   if ((spec && !pos_dev) || (q_dev == nullptr) != (q_out_dev == nullptr)) return ILRE_ERR_INVALID_ARG;
+  if (!aligned4(pos_dev)) return ILRE_ERR_ALIGNMENT;
   int64_t ks = pool->k_page_stride, vs = pool->v_page_stride;
   ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
   ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));
@@ -324,7 +329,7 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
   ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));
   ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
   if (!out_dev) return ILRE_ERR_INVALID_ARG;
-  if (!aligned16(out_dev)) return ILRE_ERR_ALIGNMENT;
+  if (!aligned16(out_dev) || !aligned4(lse_out_dev)) return ILRE_ERR_ALIGNMENT;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -368,6 +373,7 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
   ILRE_CHECK(validate_batch(h, batch, pool, true, &p.batch));
   if (batch->n_tokens == 0 || batch->n_seqs == 0 || batch->max_blocks == 0) return ILRE_OK;
   if (pool->n_pages < 1 || !lse_dev || !pool->w_dev) return ILRE_ERR_INVALID_ARG;
+  if (!aligned4(lse_dev)) return ILRE_ERR_ALIGNMENT;
   int64_t ks = pool->k_page_stride;
   ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
   ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
@@ -415,8 +421,7 @@ int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t b
     return ILRE_ERR_INVALID_ARG;
   if (batch->n_seqs == 0) return ILRE_OK;
   if (!pool->w_dev || !kept_out_dev || !new_len_out_dev) return ILRE_ERR_INVALID_ARG;
-  p.k_page_stride = pool->k_page_stride;
-  p.v_page_stride = pool->v_page_stride;
+  if (!aligned4(dst_table_dev) || !aligned4(kept_out_dev) || !aligned4(new_len_out_dev)) return ILRE_ERR_ALIGNMENT;
   int64_t ks = pool->k_page_stride, vs = pool->v_page_stride;
   ILRE_CHECK(validate_pool(h, pool->k_dev, &ks));
   ILRE_CHECK(validate_pool(h, pool->v_dev, &vs));

@@ -1,4 +1,5 @@
 """The paged-cache operators on the GPU against their definitions in 64 bits, through the Python entry points."""
+import ctypes
 import math
 
 import pytest
@@ -188,13 +189,13 @@ def test_attention_matches_64_bits(case):
 
 def test_attention_rows_that_see_nothing():
     """kv_len below the number of new tokens: the first of them see no row; a sequence without any row."""
-    b = ref.Batch([5, 200, 3, 2], [3, 150, 0, 2], 16, 2, 8, seed=5)
+    b = ref.Batch([5, 200, 3, 2, 60], [3, 150, 0, 2, 0], 16, 2, 8, seed=5)
     eng = _engine(b)
     t = b.gpu(eng)
     out, lse = eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], want_lse=True)
     want, want_lse, tol, tol_lse = ref.attention(b)
     empty = torch.isneginf(want_lse)
-    assert bool(empty[:2].all()) and bool(empty[5:55].all()) and bool(empty[205:208].all())
+    assert bool(empty[:2].all()) and bool(empty[5:55].all()) and bool(empty[205:208].all()) and bool(empty[210:].all())
     assert bool((out.cpu()[empty] == 0).all()) and torch.equal(torch.isneginf(lse.cpu()), empty)
     assert bool(((out.double().cpu() - want).abs() <= tol).all())
     assert bool(((lse.double().cpu() - want_lse).abs() <= tol_lse)[~empty].all())
@@ -430,6 +431,18 @@ def test_refused_arguments():
     odd = torch.zeros(2 * 8 * 128 + 1, dtype=BF, device="cuda")[1:].view(2, 8, 128)
     assert _code(eng.attention, t["batch"], odd, t["k_pool"], t["v_pool"]) == -5
     assert _code(eng.append, t["batch"], t["q"], t["k"], t["v"], t["pos"], _spec(rotary_dim=20), t["k_pool"], t["v_pool"]) == -2
+    # through the C call: arrays at odd addresses are refused, nothing is launched
+    from paper_2508_17892_b200.paged import IlrePagedBatch, IlrePagedPool
+    good = (2, 2, 1, 3, t["q_start"].data_ptr(), t["kv_len"].data_ptr(), t["table"].data_ptr())
+    pool = IlrePagedPool(t["k_pool"].data_ptr(), t["v_pool"].data_ptr(), t["w_pool"].data_ptr(), 0, 0, b.n_pages)
+    out, lse = torch.empty_like(t["q"]), torch.empty(2, 8, device="cuda")
+    for i in (4, 5, 6, None):
+        a = list(good)
+        if i is not None:
+            a[i] += 2
+        assert eng._lib.ilre_paged_attention(eng._h, ctypes.byref(IlrePagedBatch(*a)), t["q"].data_ptr(), 1024,
+                                             ctypes.byref(pool), out.data_ptr(), lse.data_ptr() + (2 if i is None else 0),
+                                             None) == -5
     for bad in (dict(q=t["q"][:1]), dict(q=t["q"].float()), dict(k_pool=t["k_pool"][:, :8]), dict(q=t["q"].cpu())):
         a = dict(batch=t["batch"], q=t["q"], k_pool=t["k_pool"], v_pool=t["v_pool"])
         a.update(bad)

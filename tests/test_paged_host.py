@@ -64,7 +64,7 @@ def test_rope_refusals(lib):
                      (dict(n_heads=0), -1), (dict(head_dim=120), -2), (dict(head_dim=2048), -2), (dict(dtype=2), -1),
                      (dict(n_heads=70000), -3), (dict(n_tokens=2 ** 31), -3), (dict(pos=None), -1), (dict(xp=None), -1),
                      (dict(op=None), -1), (dict(xs=255), -1), (dict(xs=260), -5), (dict(xp=odd), -5), (dict(op=odd), -5),
-                     (dict(os_=128), -1)):
+                     (dict(os_=128), -1), (dict(pos=odd), -5)):
         assert call(**kw) == code, kw
     assert lib.ilre_rope(None, x, 256, x, 256, x, 4, 2, 128, 0, 0, None) == -1
     assert call(n_tokens=0, xp=None, op=None, pos=None) == 0
