@@ -48,15 +48,6 @@ struct AttnTail {
 };
 static_assert(sizeof(AttnTail) <= kAttnTailBytes, "tail too large");
 
-// Shared-memory matrix descriptor of an operand whose contiguous dimension is M or N (here: the
-// value tile, head channels contiguous), 128-byte swizzle: 64-channel x 8-row atoms of 1024 bytes;
-// `lbo` = byte distance of the next 64 channels, `sbo` = byte distance of the next 8 rows.
-__device__ __forceinline__ uint64_t umma_desc_sw128_mn(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  const uint32_t lo = ((addr >> 4) & 0x3FFFu) | (((lbo >> 4) & 0x3FFFu) << 16);
-  const uint32_t hi = ((sbo >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29);
-  return (static_cast<uint64_t>(hi) << 32) | lo;
-}
-
 __global__ void __launch_bounds__(kAttnThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                        const __grid_constant__ CUtensorMap map_k,

@@ -7,10 +7,10 @@
 // arrive in 128-key tiles through one TMA ring; a lane of the loading warp fetches the rows that one page has in the
 // tile.  The output is kept against a reference maximum that moves only when it is outrun by 2^8.
 //
-// What bounds it: the exponentials (one per logit; a part of them as polynomials on the FMA pipe makes it slower, 431 ->
-// 436 -> 451 us with 0, 2 and 4 of 16 pairs for 1024 tokens behind 31744 rows) and the tensor pipe, of about the same
-// length.  So nothing may leave either idle: the batch's key tiles are cut into
-// equal shares, one per SM (paged_batch.cuh), and a CTA runs its pieces as one stream of tiles: ring, barriers and
+// What bounds it: the exponentials, one per logit, and the tensor pipe, of about the same length (2048 cycles per unit,
+// which takes 2900; a part of the exponentials as polynomials on the FMA pipe makes it slower, 431 -> 436 -> 451 us with 0, 2
+// and 4 of 16 pairs for 1024 tokens behind 31744 rows).  So nothing may leave either idle: the batch's key tiles are cut
+// into equal shares, one per SM (paged_batch.cuh), and a CTA runs its pieces as one stream of tiles: ring, barriers and
 // tensor memory go on from piece to piece, the next piece's first logits are computed while the last one's output is
 // written.  An item that the cut divides leaves 32-bit partial outputs, which a second kernel joins in the order of the
 // CTAs.
@@ -40,7 +40,7 @@ struct ChunkTail {
   uint64_t kv_empty[kStages];
   uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2], o_full[2];      // per stream
   PlanStart plan;
-  PieceWalk<HeadTiles> walk[2 * kSoftmaxWarps];                     // one per softmax warp
+  PieceWalk<HeadTiles> walk[2 * kSoftmaxWarps];          // one per softmax warp
   uint32_t tmem_base;
   int abort_flag;
   int v_landed;                                          // value tiles that the PV thread has seen arrive
@@ -49,15 +49,6 @@ struct ChunkTail {
 constexpr size_t kSmem = static_cast<size_t>(4 + kStages) * kTileBytes + sizeof(ChunkTail);
 static_assert(kSmem <= 232448, "shared memory");
 
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  const uint32_t lo = ((addr >> 4) & 0x3FFFu) | (((lbo >> 4) & 0x3FFFu) << 16);
-  const uint32_t hi = ((sbo >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29);
-  return (static_cast<uint64_t>(hi) << 32) | lo;
-}
-template <bool kF16>
-__host__ __device__ constexpr uint32_t idesc(int M, int N) {      // operand types: bits 7 and 10, f16 0, bf16 1
-  return kF16 ? umma_idesc_bf16(M, N) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(M, N);
-}
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -192,8 +183,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // asked for only once the item before it in its slot, three items earlier, is known to have arrived: the PV
     // thread knows (P of its tile is made from that tile's keys), the S thread asks for the count of value tiles.
     if (lane == 0 && run) {
-      constexpr uint32_t idesc_s = idesc<kF16>(128, 128);
-      constexpr uint32_t idesc_o = idesc<kF16>(128, 128) | (1u << 16);     // B = V: channels contiguous
+      constexpr uint32_t idesc_s = kF16 ? umma_idesc_f16(128, 128) : umma_idesc_bf16(128, 128);
+      constexpr uint32_t idesc_o = idesc_s | (1u << 16);                   // B = V: channels contiguous
       const bool s_role = (warp == 1);
       volatile int* v_landed = &tail->v_landed;
       PieceWalk<HeadTiles> w;
@@ -253,7 +244,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                   for (int ks = 0; ks < 4; ++ks)
                     umma_bf16(tmem_base + 256 + x * 128, umma_desc_sw128(px + kb * kHalf + ks * 32),
-                              desc_mn(v_s + (kb * 64 + ks * 16) * 128, kHalf, 1024), idesc_o, (i | kb | ks) != 0);
+                              umma_desc_sw128_mn(v_s + (kb * 64 + ks * 16) * 128, kHalf, 1024), idesc_o, (i | kb | ks) != 0);
                 umma_commit(smem_u32(&tail->p_empty[x]));
                 next[x] = i + 1;
                 progress = true;

@@ -38,8 +38,8 @@ constexpr int kFirstSum = 1 + kIssuers;                  // warp 0 loads, then t
 constexpr int kThreads = 32 * kFirstSum + kGroups * 128;
 
 // A piece as the loading warp hands it to the others.  The ring is safe without a barrier of its own: a place is
-// written again 16 pieces later, behind the wait for the MMAs of a piece at most 6 before, which waited for accumulators that
-// every group has read, of pieces at least 3 behind the place's.
+// written again 16 pieces later, behind the wait for both threads' MMAs of the piece two before that, which waited for
+// accumulators that every group has read, of pieces at least 9 behind the place's.
 struct Job {
   int kt, row_tile, count, flags;          // key tile, first row tile, units (0: the end); kCut, kOfFirst
   int q0, n, kv, place;                    // span; head + n_kv * sequence
@@ -214,7 +214,7 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     }
   } else if (warp < kFirstSum) {
     {
-      const uint32_t idesc = kF16 ? umma_idesc_bf16(128, n_cols) & ~((1u << 7) | (1u << 10)) : umma_idesc_bf16(128, n_cols);
+      constexpr uint32_t idesc = kF16 ? umma_idesc_f16(128, n_cols) : umma_idesc_bf16(128, n_cols);
       // An issuing thread is held until the tensor pipe takes its instructions, and its waits and commits leave the
       // pipe idle (128 keys by 128 rows take it some 500 cycles, one thread 1340): two of them take turns.
       const int parity = warp - 1;                       // of its units, and the accumulators 2 parity, 2 parity + 1

@@ -229,10 +229,24 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t addr) {
   return (static_cast<uint64_t>(hi) << 32) | lo;
 }
 
+// Shared-memory matrix descriptor of an operand whose contiguous dimension is M or N (a value tile,
+// head channels contiguous), 128-byte swizzle: 64-channel x 8-row atoms of 1024 bytes;
+// `lbo` = byte distance of the next 64 channels, `sbo` = byte distance of the next 8 rows.
+__device__ __forceinline__ uint64_t umma_desc_sw128_mn(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  const uint32_t lo = ((addr >> 4) & 0x3FFFu) | (((lbo >> 4) & 0x3FFFu) << 16);
+  const uint32_t hi = ((sbo >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29);
+  return (static_cast<uint64_t>(hi) << 32) | lo;
+}
+
 // Instruction descriptor of kind::f16: bf16 x bf16 -> fp32, both operands K-major.
 __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// The same for f16 x f16 -> fp32 (operand types: bits 7 and 10).
+__host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
+  return umma_idesc_bf16(M, N) & ~((1u << 7) | (1u << 10));
 }
 
 // D[tmem] (+)= A[smem] * B[smem]^T, issued by one thread.

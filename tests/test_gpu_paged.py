@@ -668,3 +668,41 @@ def _as_now(b, small, q, out):
     fresh.k_pool, fresh.v_pool = t["k_pool"].cpu(), t["v_pool"].cpu()
     eng.close()
     return fresh
+
+
+def test_two_caches_on_two_streams():
+    """Two handles at work at the same time, and their captured steps replayed side by side."""
+    made = []
+    for seed, (q_len, kv_len) in enumerate((([1, 1, 30], [3000, 700, 900]), ([200, 1], [900, 2500]))):
+        b = ref.Batch(q_len, kv_len, 32, 4, 16, seed=20 + seed)
+        eng = _engine(b)
+        t = b.gpu(eng)
+        out, lse = torch.empty_like(t["q"]), torch.empty(b.n_tokens, 16, device="cuda")
+        w = torch.zeros_like(t["w_pool"])
+
+        def step(eng=eng, t=t, out=out, lse=lse, w=w):
+            eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], out=out, lse=lse)
+            eng.accumulate(t["batch"], t["q"], lse, t["k_pool"], w)
+
+        step()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in (out, lse, w)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        made.append((eng, step, (out, lse, w), want, graph, torch.cuda.Stream()))
+    for replay in (False, True):
+        for eng, step, got, want, graph, stream in made:
+            for x in got:
+                x.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for eng, step, got, want, graph, stream in made:
+                with torch.cuda.stream(stream):
+                    got[2].zero_()
+                    graph.replay() if replay else step()
+        torch.cuda.synchronize()
+        for eng, step, got, want, graph, stream in made:
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+    for eng, *_ in made:
+        _close(eng)
