@@ -110,28 +110,17 @@ def _ints(t: torch.Tensor, index: int, n: int) -> None:
     assert t.get_device() == index and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous()
 
 
-class _OnStream:
-    """The stream of a call.  Where the caller names one, tensors made inside are its own and the caller's
-    tensors are marked as in use by it; without a name it is the device's current one."""
+def _on_stream(stream: torch.cuda.Stream, tensors):
+    """The named stream of a call: current inside, so tensors made inside are its own; the caller's tensors are
+    marked as in use by it."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return torch.cuda.stream(stream)
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], tensors):
-        self._ctx = None
-        if stream is None:
-            self.raw = torch._C._cuda_getCurrentRawStream(device.index)       # (a Stream object takes microseconds)
-            return
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-        self.raw = stream.cuda_stream
-        self._ctx = torch.cuda.stream(stream)
 
-    def __enter__(self):
-        if self._ctx is not None:
-            self._ctx.__enter__()
-        return self.raw
-
-    def __exit__(self, *exc):
-        return self._ctx.__exit__(*exc) if self._ctx is not None else None
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)     # (a Stream object takes microseconds)
 
 
 def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: bool = False,
@@ -140,23 +129,25 @@ def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: b
 
     ``out`` may be ``x``.  ``transposed`` applies the transposed map: the gradient of ``rope`` with
     respect to x is ``rope(grad, positions, spec, transposed=True)``."""
+    if stream is not None:
+        with _on_stream(stream, (x, positions, out)):
+            return rope(x, positions, spec, transposed, out)
     dtype, index = x.dtype, x.get_device()
     assert index >= 0 and dtype in _DTYPES
     n, heads, dim = x.shape
     _ints(positions, index, n)
     x_stride = _rows(x, index, dtype, heads, dim)
-    with _OnStream(x.device, stream, (x, positions, out)) as st:
-        if out is None:
-            out = torch.empty(n, heads, dim, dtype=dtype, device=x.device)
-        out_stride = _rows(out, index, dtype, heads, dim)
-        assert out.shape[0] == n
-        args = (spec.ref, x.data_ptr(), x_stride, out.data_ptr(), out_stride, positions.data_ptr(), n, heads, dim,
-                _DTYPES[dtype], int(transposed), st)
-        if torch.cuda.current_device() == index:
+    if out is None:
+        out = torch.empty(n, heads, dim, dtype=dtype, device=x.device)
+    out_stride = _rows(out, index, dtype, heads, dim)
+    assert out.shape[0] == n
+    args = (spec.ref, x.data_ptr(), x_stride, out.data_ptr(), out_stride, positions.data_ptr(), n, heads, dim,
+            _DTYPES[dtype], int(transposed), _raw_stream(index))
+    if torch.cuda.current_device() == index:
+        rc = load_library().ilre_rope(*args)
+    else:
+        with torch.cuda.device(index):
             rc = load_library().ilre_rope(*args)
-        else:
-            with torch.cuda.device(x.device):
-                rc = load_library().ilre_rope(*args)
     if rc != 0:
         raise IlreError(rc, "ilre_rope")
     return out
@@ -216,16 +207,16 @@ class PagedCache:
         assert q.shape[0] == n and (n == 0 or batch.q_start is not None)
         return _rows(q, self._index, self.dtype, self._n_q, self._dim)
 
-    def _check(self, rc: int, what: str) -> None:
-        if rc != 0:
-            raise IlreError(rc, what)
-
     def append(self, batch: PagedBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                positions: Optional[torch.Tensor], spec: Optional[RopeSpec], k_pool: torch.Tensor, v_pool: torch.Tensor,
                w_pool: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
         """k turned and v copied to the new tokens' rows, their weights cleared; returns q turned (``q_out``, which
         may be q; made here if not given).  spec None: nothing is turned."""
+        if stream is not None:
+            with _on_stream(stream, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start, batch.kv_len,
+                                     batch.block_table)):
+                return self.append(batch, q, k, v, positions, spec, k_pool, v_pool, w_pool, q_out)
         n, n_kv, dim = batch.n_tokens, self._page_shape[1], self._dim
         assert k.shape[0] == n and v.shape[0] == n
         k_stride = _rows(k, self._index, self.dtype, n_kv, dim)
@@ -234,20 +225,19 @@ class PagedCache:
         if positions is not None:
             _ints(positions, self._index, n)
         pool = self._pool(k_pool, v_pool, w_pool)
-        with _OnStream(self.device, stream, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start,
-                                             batch.kv_len, batch.block_table)) as st:
-            q_stride = q_out_stride = 0
-            if q is not None:
-                q_stride = self._q(batch, q)
-                if q_out is None:
-                    q_out = torch.empty(n, self._n_q, dim, dtype=q.dtype, device=q.device)
-                q_out_stride = self._q(batch, q_out)
-            else:
-                assert q_out is None
-            self._check(self._lib.ilre_paged_append(
-                self._h, batch.ref, spec.ref if spec is not None else None,
-                _ptr(positions), _ptr(q), q_stride, _ptr(q_out), q_out_stride, k.data_ptr(), k_stride, v.data_ptr(),
-                v_stride, ctypes.byref(pool), st), "ilre_paged_append")
+        q_stride = q_out_stride = 0
+        if q is not None:
+            q_stride = self._q(batch, q)
+            if q_out is None:
+                q_out = torch.empty(n, self._n_q, dim, dtype=q.dtype, device=q.device)
+            q_out_stride = self._q(batch, q_out)
+        else:
+            assert q_out is None
+        rc = self._lib.ilre_paged_append(
+            self._h, batch.ref, spec.ref if spec is not None else None, _ptr(positions), _ptr(q), q_stride, _ptr(q_out),
+            q_out_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, ctypes.byref(pool), _raw_stream(self._index))
+        if rc != 0:
+            raise IlreError(rc, "ilre_paged_append")
         return q_out
 
     def attention(self, batch: PagedBatch, q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
@@ -255,21 +245,22 @@ class PagedCache:
                   stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """Every new token over its sequence's cached rows up to itself: (out like q, lse fp32 [n_tokens, n_q_heads]
         or None).  Rows of tokens that belong to no sequence are left as they are."""
+        if stream is not None:
+            with _on_stream(stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len, batch.block_table)):
+                return self.attention(batch, q, k_pool, v_pool, out, lse, want_lse)
         q_stride = self._q(batch, q)
         pool = self._pool(k_pool, v_pool, None)
         shape = (batch.n_tokens, self._n_q, self._dim)
-        with _OnStream(self.device, stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len,
-                                             batch.block_table)) as st:
-            if out is None:
-                out = torch.empty(shape, dtype=q.dtype, device=q.device)
-            if lse is None and want_lse:
-                lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
-            assert out.shape == shape and out.dtype == self.dtype and out.is_contiguous()
-            assert out.get_device() == self._index
-            self._lse(batch, lse)
-            self._check(self._lib.ilre_paged_attention(
-                self._h, batch.ref, q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
-                _ptr(lse), st), "ilre_paged_attention")
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        if lse is None and want_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+        assert out.shape == shape and out.dtype == self.dtype and out.is_contiguous() and out.get_device() == self._index
+        self._lse(batch, lse)
+        rc = self._lib.ilre_paged_attention(self._h, batch.ref, q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
+                                            _ptr(lse), _raw_stream(self._index))
+        if rc != 0:
+            raise IlreError(rc, "ilre_paged_attention")
         return out, lse
 
     def _lse(self, batch: PagedBatch, lse: Optional[torch.Tensor]) -> None:
@@ -280,15 +271,17 @@ class PagedCache:
                    w_pool: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Adds to w_pool the attention weight that every cached row received from the batch's new tokens (q and lse
         as ``attention`` had and returned them).  Returns w_pool."""
+        if stream is not None:
+            with _on_stream(stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len, batch.block_table)):
+                return self.accumulate(batch, q, lse, k_pool, w_pool)
         q_stride = self._q(batch, q)
         assert lse is not None and w_pool is not None
         self._lse(batch, lse)
         pool = self._pool(k_pool, None, w_pool)
-        with _OnStream(self.device, stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len,
-                                             batch.block_table)) as st:
-            self._check(self._lib.ilre_paged_accumulate(
-                self._h, batch.ref, q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
-                st), "ilre_paged_accumulate")
+        rc = self._lib.ilre_paged_accumulate(self._h, batch.ref, q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
+                                             _raw_stream(self._index))
+        if rc != 0:
+            raise IlreError(rc, "ilre_paged_accumulate")
         return w_pool
 
     def evict(self, batch: PagedBatch, budget: int, n_sink: int, n_recent: int, k_pool: torch.Tensor,
@@ -299,25 +292,30 @@ class PagedCache:
         moved to rows 0, 1, ... of its own pages or of dst_table's (int32 [n_seqs, dst_blocks]).  Returns (kept
         int32 [n_seqs, n_kv_heads or 1, budget], ascending, -1 behind a shorter sequence; new_len int32 [n_seqs],
         which may be batch.kv_len)."""
-        n = batch.kv_len.numel()
+        if stream is not None:
+            with _on_stream(stream, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len, batch.block_table)):
+                return self.evict(batch, budget, n_sink, n_recent, k_pool, v_pool, w_pool, per_head, dst_table, kept, new_len)
+        n, index = batch.kv_len.numel(), self._index
         shape = (n, self._page_shape[1] if per_head else 1, budget)
         assert budget >= 1 and w_pool is not None
         pool = self._pool(k_pool, v_pool, w_pool)
+        dst_blocks = 0
         if dst_table is not None:
-            assert dst_table.device == self.device and dst_table.dtype == torch.int32 and dst_table.is_contiguous()
+            assert dst_table.get_device() == index and dst_table.dtype == torch.int32 and dst_table.is_contiguous()
             assert dst_table.dim() == 2 and dst_table.shape[0] == n
-        with _OnStream(self.device, stream, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len,
-                                             batch.block_table)) as st:
-            if kept is None:
-                kept = torch.empty(shape, dtype=torch.int32, device=self.device)
-            if new_len is None:
-                new_len = torch.empty(n, dtype=torch.int32, device=self.device)
-            for t, want in ((kept, shape), (new_len, (n,))):
-                assert t.shape == want and t.dtype == torch.int32 and t.is_contiguous() and t.get_device() == self._index
-            self._check(self._lib.ilre_paged_evict(
-                self._h, batch.ref, budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
-                _ptr(dst_table), dst_table.shape[1] if dst_table is not None else 0, kept.data_ptr(),
-                new_len.data_ptr(), st), "ilre_paged_evict")
+            dst_blocks = dst_table.shape[1]
+        if kept is None:
+            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+        else:
+            assert kept.shape == shape and kept.dtype == torch.int32 and kept.is_contiguous() and kept.get_device() == index
+        if new_len is None:
+            new_len = torch.empty(n, dtype=torch.int32, device=self.device)
+        else:
+            _ints(new_len, index, n)
+        rc = self._lib.ilre_paged_evict(self._h, batch.ref, budget, n_sink, n_recent, int(per_head), ctypes.byref(pool),
+                                        _ptr(dst_table), dst_blocks, kept.data_ptr(), new_len.data_ptr(), _raw_stream(index))
+        if rc != 0:
+            raise IlreError(rc, "ilre_paged_evict")
         return kept, new_len
 
     # -- diagnostics -------------------------------------------------------------------
@@ -325,7 +323,9 @@ class PagedCache:
         return self._lib.ilre_paged_status(self._h)
 
     def check_status(self) -> None:
-        self._check(self.status(), "ilre_paged_status")
+        rc = self.status()
+        if rc != 0:
+            raise IlreError(rc, "ilre_paged_status")
 
     def check_guards(self) -> int:
         """Number of workspace buffers whose guard zone was written to (0 = none); synchronises."""
