@@ -434,7 +434,7 @@ int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t b
   p.per_head = per_head != 0; p.dst_table = dst_table_dev; p.dst_blocks = dst_blocks;
   p.kept = kept_out_dev; p.new_len = new_len_out_dev; p.n_keep = h->n_keep;
   if (dst_table_dev && evict_copy_blocks(p) > 2147483647LL) return ILRE_ERR_CAPACITY;
-  ILRE_CUDA(launch_evict(p, st));
+  ILRE_CUDA(launch_evict(p, h->n_sm, st));
   h->last_launches = 2;
   return ILRE_OK;
 }

@@ -26,7 +26,6 @@ constexpr int kSelBins = 2048;
 constexpr int kSelKeep = 44032;                          // keys of a CTA that shared memory takes, at most
 constexpr int kMoveThreads = 256;
 constexpr int kMoveRows = 64;                            // rows of a CTA that copies to other pages
-constexpr int kMoveFlight = 8;                           // rows of a thread in flight, in place
 constexpr int kMoveCols = 8;                             // columns of a head: 4 of keys, 4 of values
 
 // Row t's key: larger is heavier; the sum over the heads is formed in double and rounded once, so its value does
@@ -246,7 +245,10 @@ evict_copy_kernel(const __grid_constant__ EvictParams p) {
 }
 
 // In place: CTA x of a head has column x of its keys or values, the last one its weights.  Rows that stay lead the list
-// (kept[i] = i) and are passed over.
+// (kept[i] = i) and are passed over.  kMoveFlight: rows of a thread in flight, 8 where the launch leaves SMs
+// to spare and a CTA's own rate counts, 2 where many CTAs share them (one request of 4608 rows 38 us with 8, 42 with 2; 16
+// prompts of 6000 to 14000 rows 209 with 8, 138 with 2).
+template <int kMoveFlight>
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(const __grid_constant__ EvictParams p) {
   const int col = blockIdx.x, g = blockIdx.y, seq = blockIdx.z;
@@ -336,7 +338,7 @@ cudaError_t init_evict() {
                               static_cast<int>(kSelKeep * 4 + sizeof(SelShared)));
 }
 
-cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
+cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st) {
   const int lists = p.per_head ? p.n_kv : 1;
   const long long rows = static_cast<long long>(p.batch.max_blocks) << p.batch.page_shift;
   // Few CTAs for short lists: what a CTA reads of the others' histograms grows with their number (24 KB each, the
@@ -364,7 +366,9 @@ cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
   if (p.dst_table)
     return launch_after_previous(evict_copy_kernel, dim3(static_cast<unsigned>(evict_copy_blocks(p)), 1, p.batch.n_seqs),
                                  kMoveThreads, 0, st, p);
-  return launch_after_previous(evict_move_kernel, dim3(kMoveCols + 1, p.n_kv, p.batch.n_seqs), kMoveThreads, 0, st, p);
+  const dim3 grid(kMoveCols + 1, p.n_kv, p.batch.n_seqs);
+  const bool many = static_cast<long long>(grid.x) * grid.y * grid.z > 2ll * n_sm;
+  return launch_after_previous(many ? evict_move_kernel<2> : evict_move_kernel<8>, grid, kMoveThreads, 0, st, p);
 }
 
 }  // namespace ilre

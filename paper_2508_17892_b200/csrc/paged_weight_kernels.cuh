@@ -50,6 +50,6 @@ cudaError_t launch_paged_weights(const CUtensorMap& map_q, const CUtensorMap& ma
 cudaError_t launch_paged_weight_rows(const CUtensorMap& map_k, const PagedWeightParams& p, bool f16, int n_sm,
                                      cudaStream_t st);
 long long evict_copy_blocks(const EvictParams& p);     // CTAs per sequence of the copy to other pages, < 2^31
-cudaError_t launch_evict(const EvictParams& p, cudaStream_t st);
+cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st);
 
 }  // namespace ilre
