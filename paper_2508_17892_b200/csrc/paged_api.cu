@@ -177,7 +177,8 @@ float softmax_scale() { return static_cast<float>(1.4426950408889634 / std::sqrt
 
 // Sequences whose rows (new tokens x heads of a group) fit one tile of 16 are bound by the reading of the cache and
 // go to the row kernels; the others' rows share a key tile in the tensor-core kernels.  The launches follow from what
-// the host knows: one sequence has one kind, and max_q_len may rule out the second.
+// the host knows: one sequence has one kind, and max_q_len may rule out the second.  (Eight sequences of 16000 rows,
+// 32 / 8 heads: 4 new tokens 96 us by rows; 5 tokens 146 us by rows, in two tiles, 111 us in the chunk kernel.)
 struct KernelChoice {
   int row_tokens;                                        // most new tokens of the first kind; 0: more than 16 heads
   bool rows, chunks;
