@@ -476,10 +476,10 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out);
  * New tokens into the cache: k [n_tokens][n_kv_heads][128] is rotated by the tokens' positions (ilre_rope)
  * and v copied to the rows of the new tokens, their accumulated weights (w_dev, if given) are set to
  * 0, and q [n_tokens][n_q_heads][128] is rotated into q_out.  Strides in elements from token to token
- * (multiples of 8; q_out may be q with its stride).  q_dev and q_out_dev may both be NULL, and spec NULL copies
- * without a rotation (pos_dev may then be NULL).  Positions are given apart from the rows because after an
- * eviction they differ.  kv_len[i] >= n_i (else the sequence is left out and reported); rows that are
- * written belong to one sequence, on one page.
+ * (multiples of 8; q_out may be q with its stride, else they do not overlap).  q_dev and q_out_dev may both
+ * be NULL, and spec NULL copies without a rotation (pos_dev may then be NULL).  Positions are given apart from
+ * the rows because after an eviction they differ.  kv_len[i] >= n_i (else the sequence is left out and
+ * reported); rows that are written belong to one sequence, on one page.
  */
 int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const ilre_rope_spec_t* spec,
                       const int32_t* pos_dev, const void* q_dev, int64_t q_stride, void* q_out_dev,
@@ -490,11 +490,11 @@ int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const il
  * Attention of the new tokens over the cache (Eq. 2's step for every layer behind the compression):
  *   out[j, h, :] = sum_t softmax_t(q[j, h, :] . k[t, kv(h), :] / sqrt(128)) v[t, kv(h), :],  t visible to j
  *   lse_out[j, h] = ln sum_t exp(q . k / sqrt(128))      (fp32 [n_tokens][n_q_heads], NULL to skip)
- * q_dev [n_tokens][n_q_heads][128] with q_stride elements from token to token, out_dev contiguous.  A token
- * that sees nothing (kv_len[i] < n_i) gets zeros and lse -infinity.  Rows at kv_len[i] and beyond may hold
- * anything, NaN included; values of rows below it must be finite.  Pages may be shared.  Products on
- * the tensor cores, fp32 sums; the probabilities are rounded to the cache's type before they multiply
- * the values, as the output is.
+ * q_dev [n_tokens][n_q_heads][128] with q_stride elements from token to token, out_dev contiguous and apart
+ * from q_dev.  A token that sees nothing (kv_len[i] < n_i) gets zeros and lse -infinity.  Rows at kv_len[i]
+ * and beyond may hold anything, NaN included; keys and values of rows below it must be finite.  Pages may be
+ * shared.  Products on the tensor cores, fp32 sums; the probabilities are rounded to the cache's type before
+ * they multiply the values, as the output is.
  */
 int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev,
                          int64_t q_stride, const ilre_paged_pool_t* pool, void* out_dev,
@@ -522,14 +522,16 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
  * (NaN counts as the largest, zeros of either sign as equal; lower ones rank below).
  *   kept_out_dev     int32 [n_seqs][per_head ? n_kv_heads : 1][budget]: kept rows ascending, then -1
  *   new_len_out_dev  int32 [n_seqs]: min(kv_len, budget); may be kv_len_dev itself
- * q_start_dev is not read (may be NULL).  n_sink + n_recent <= budget (ILRE_ERR_BUDGET).
+ * q_start_dev is not read (may be NULL).  n_sink + n_recent <= budget (ILRE_ERR_BUDGET)
+ * < 2^31 - 4097 (ILRE_ERR_CAPACITY).
  */
 int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t budget, int32_t n_sink,
                      int32_t n_recent, int32_t per_head, const ilre_paged_pool_t* pool,
                      const int32_t* dst_table_dev, int32_t dst_blocks, int32_t* kept_out_dev,
                      int32_t* new_len_out_dev, void* cuda_stream);
 
-/* As ilre_recall_status, _last_launch_count, _check_guards and _destroy. */
+/* As ilre_recall_status (but it waits for the whole device: graphs that hold the handle's calls may run on any
+ * stream), _last_launch_count, _check_guards and _destroy. */
 int ilre_paged_status(ilre_paged_t* h);
 int ilre_paged_last_launch_count(ilre_paged_t* h);
 int ilre_paged_check_guards(ilre_paged_t* h);

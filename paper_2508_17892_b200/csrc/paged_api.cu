@@ -33,7 +33,6 @@ struct ilre_paged {
   int32_t* n_keep;                      // rows that an eviction keeps of each sequence
   int* status;
   int last_launches;
-  cudaStream_t last_stream;
 };
 
 namespace {
@@ -146,6 +145,17 @@ int validate_rows(const void* base, int64_t stride, int64_t heads, int head_dim)
   return ILRE_OK;
 }
 
+// Rows turned in place: every thread writes what it read, so the strides must agree.
+int validate_in_place(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t n) {
+  return in == out && in_stride != out_stride && n > 1 ? ILRE_ERR_INVALID_ARG : ILRE_OK;
+}
+
+// Query rows are read by many CTAs while others write their output.
+bool overlap(const void* q, int64_t q_stride, const void* out, int64_t n_tokens, int64_t row) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(q), b = reinterpret_cast<uintptr_t>(out);
+  return a < b + static_cast<uintptr_t>(n_tokens * row) * 2 && b < a + static_cast<uintptr_t>((n_tokens - 1) * q_stride + row) * 2;
+}
+
 // A pool as {channel, kv head, row of the page, page}, boxes of 64 channels of one head by box_rows rows.
 bool encode_pool(const ilre_paged* h, CUtensorMap* map, const void* base, int64_t page_stride, int n_pages,
                  int box_rows) {
@@ -216,6 +226,7 @@ int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride,
   if (!aligned4(pos_dev)) return ILRE_ERR_ALIGNMENT;
   ILRE_CHECK(validate_rows(x_dev, x_stride, n_heads, head_dim));
   ILRE_CHECK(validate_rows(out_dev, out_stride, n_heads, head_dim));
+  ILRE_CHECK(validate_in_place(x_dev, x_stride, out_dev, out_stride, n_tokens));
   int dev = 0, n_sm = 0;
   ILRE_CUDA(cudaGetDevice(&dev));
   ILRE_CUDA(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
@@ -302,11 +313,11 @@ int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const il
   if (q_dev) {
     ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
     ILRE_CHECK(validate_rows(q_out_dev, q_out_stride, h->cfg.n_q_heads, kDim));
+    ILRE_CHECK(validate_in_place(q_dev, q_stride, q_out_dev, q_out_stride, batch->n_tokens));
   }
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  h->last_stream = st;
   p.q = RopeRows{q_dev, q_out_dev, q_stride, q_out_stride, q_dev ? h->cfg.n_q_heads : 0};
   p.k = RopeRows{k_dev, pool->k_dev, k_stride, 0, h->cfg.n_kv_heads};
   p.v = RopeRows{v_dev, pool->v_dev, v_stride, 0, h->cfg.n_kv_heads};
@@ -331,10 +342,11 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
   ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
   if (!out_dev) return ILRE_ERR_INVALID_ARG;
   if (!aligned16(out_dev) || !aligned4(lse_out_dev)) return ILRE_ERR_ALIGNMENT;
+  if (overlap(q_dev, q_stride, out_dev, batch->n_tokens, static_cast<int64_t>(h->cfg.n_q_heads) * kDim))
+    return ILRE_ERR_INVALID_ARG;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  h->last_stream = st;
   p.q = q_dev; p.q_stride = q_stride; p.out = out_dev; p.lse = lse_out_dev;
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
@@ -381,7 +393,6 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  h->last_stream = st;
   p.lse = lse_dev; p.w = pool->w_dev;
   p.n_q = h->cfg.n_q_heads; p.n_kv = h->cfg.n_kv_heads; p.group = p.n_q / p.n_kv;
   p.c2 = softmax_scale();
@@ -418,6 +429,7 @@ int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t b
   ILRE_CHECK(validate_batch(h, batch, pool, false, &p.batch));
   if (budget < 1 || n_sink < 0 || n_recent < 0) return ILRE_ERR_INVALID_ARG;
   if (static_cast<long long>(n_sink) + n_recent > budget) return ILRE_ERR_BUDGET;
+  if (budget >= 2147483647 - 4096) return ILRE_ERR_CAPACITY;       // the kernels step over it by up to 4096 at a time
   if (dst_table_dev && (dst_blocks < 1 || static_cast<long long>(dst_blocks) * h->cfg.page_size < budget))
     return ILRE_ERR_INVALID_ARG;
   if (batch->n_seqs == 0) return ILRE_OK;
@@ -429,7 +441,6 @@ int ilre_paged_evict(ilre_paged_t* h, const ilre_paged_batch_t* batch, int32_t b
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  h->last_stream = st;
   p.k = pool->k_dev; p.v = pool->v_dev; p.w = pool->w_dev; p.k_page_stride = ks; p.v_page_stride = vs;
   p.n_kv = h->cfg.n_kv_heads; p.budget = budget; p.n_sink = n_sink; p.n_recent = n_recent;
   p.per_head = per_head != 0; p.dst_table = dst_table_dev; p.dst_blocks = dst_blocks;
@@ -444,13 +455,14 @@ int ilre_paged_status(ilre_paged_t* h) {
   if (!h) return ILRE_ERR_INVALID_ARG;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;
-  ILRE_CUDA(cudaStreamSynchronize(h->last_stream));
+  ILRE_CUDA(cudaDeviceSynchronize());                    // the device: graphs with the handle's calls run on any stream
   int word = 0;
   ILRE_CUDA(cudaMemcpy(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost));
   if (word == 0) return ILRE_OK;
   ILRE_CUDA(cudaMemset(h->status, 0, sizeof(int)));
   // a kernel that gave up (now or behind another fault) may not have counted all arrivals
   ILRE_CUDA(cudaMemset(h->arrived, 0, static_cast<size_t>(h->n_sm) * kRowCtasPerSm * sizeof(uint32_t)));
+  ILRE_CUDA(cudaDeviceSynchronize());                    // before a later call, whose stream may not wait for this one
   return (word == kDevBadLengths || word == kDevBadPage) ? ILRE_ERR_BATCH : ILRE_ERR_DEVICE_WAIT;
 }
 

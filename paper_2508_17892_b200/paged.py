@@ -7,7 +7,7 @@ weight that each row receives and evicts by it; ``rope`` turns a tensor of heads
 from __future__ import annotations
 
 import ctypes
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 from typing import Optional, Tuple
 
 import torch
@@ -76,6 +76,9 @@ class RopeSpec:
             self.low, self.high, self.attn_factor))
         object.__setattr__(self, "ref", ctypes.byref(self._c))
 
+    def __reduce__(self):                                  # copies and pickles hold the fields, not the C struct
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
 
 @dataclass(frozen=True)
 class PagedBatch:
@@ -91,6 +94,7 @@ class PagedBatch:
             self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1], _ptr(self.q_start),
             self.kv_len.data_ptr(), self.block_table.data_ptr()))
         object.__setattr__(self, "ref", ctypes.byref(self._c))
+        object.__setattr__(self, "index", self.kv_len.get_device())
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -195,7 +199,8 @@ class PagedCache:
         assert step[1:] == self._page_stride or shape[0] == 0 or t[0].is_contiguous()
         return step[0] if shape[0] > 1 else 0
 
-    def _pool(self, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
+    def _pool(self, batch: PagedBatch, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
+        assert batch.index == self._index                  # its arrays are read on the handle's device
         n_pages = k.shape[0]
         shape = (n_pages,) + self._page_shape
         assert w is None or (w.shape == (n_pages,) + self._weight_shape and w.dtype == torch.float32 and
@@ -224,7 +229,7 @@ class PagedCache:
         assert spec is None or positions is not None
         if positions is not None:
             _ints(positions, self._index, n)
-        pool = self._pool(k_pool, v_pool, w_pool)
+        pool = self._pool(batch, k_pool, v_pool, w_pool)
         q_stride = q_out_stride = 0
         if q is not None:
             q_stride = self._q(batch, q)
@@ -249,7 +254,7 @@ class PagedCache:
             with _on_stream(stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len, batch.block_table)):
                 return self.attention(batch, q, k_pool, v_pool, out, lse, want_lse)
         q_stride = self._q(batch, q)
-        pool = self._pool(k_pool, v_pool, None)
+        pool = self._pool(batch, k_pool, v_pool, None)
         shape = (batch.n_tokens, self._n_q, self._dim)
         if out is None:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)
@@ -277,7 +282,7 @@ class PagedCache:
         q_stride = self._q(batch, q)
         assert lse is not None and w_pool is not None
         self._lse(batch, lse)
-        pool = self._pool(k_pool, None, w_pool)
+        pool = self._pool(batch, k_pool, None, w_pool)
         rc = self._lib.ilre_paged_accumulate(self._h, batch.ref, q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
                                              _raw_stream(self._index))
         if rc != 0:
@@ -298,7 +303,7 @@ class PagedCache:
         n, index = batch.kv_len.numel(), self._index
         shape = (n, self._page_shape[1] if per_head else 1, budget)
         assert budget >= 1 and w_pool is not None
-        pool = self._pool(k_pool, v_pool, w_pool)
+        pool = self._pool(batch, k_pool, v_pool, w_pool)
         dst_blocks = 0
         if dst_table is not None:
             assert dst_table.get_device() == index and dst_table.dtype == torch.int32 and dst_table.is_contiguous()

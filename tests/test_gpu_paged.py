@@ -706,3 +706,58 @@ def test_two_caches_on_two_streams():
             assert all(torch.equal(x, y) for x, y in zip(got, want))
     for eng, *_ in made:
         _close(eng)
+
+
+# ---- calls that only the documentation makes -------------------------------------------------------------
+
+def test_status_of_a_graph_on_another_stream():
+    """The last call by hand is on the current stream, the replay with a bad length on a side stream behind long
+    work: the status still tells."""
+    b = ref.Batch([1, 1], [40, 40], 16, 2, 8, seed=4)
+    eng = _engine(b)
+    t = b.gpu(eng)
+    out = torch.empty_like(t["q"])
+    eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], out=out)
+    t["kv_len"][1] = -1
+    eng.append(t["batch"], None, t["k"][:2], t["v"][:2], None, None, t["k_pool"], t["v_pool"])
+    assert eng.status() == -10
+    torch.cuda.synchronize()
+    side, big = torch.cuda.Stream(), torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(40):                                  # some 10 ms
+            big.add_(1.0)
+        graph.replay()
+    assert eng.status() == -10
+    _close(eng)
+
+
+def test_refused_overlaps_and_budgets():
+    from paper_2508_17892_b200.paged import PagedBatch
+    b = ref.Batch([2, 2], [40, 40], 16, 2, 8)
+    eng = _engine(b)
+    t = b.gpu(eng)
+    q = torch.zeros(8, 8, 128, dtype=BF, device="cuda")
+    for at in (0, 1, 3):                                     # the output over the queries, or over some of them
+        assert _code(eng.attention, t["batch"], q[:4], t["k_pool"], t["v_pool"], out=q[at:at + 4]) == -1
+    eng.attention(t["batch"], q[:4], t["k_pool"], t["v_pool"], out=q[4:])
+    wide = torch.zeros(4, 16, 128, dtype=BF, device="cuda")
+    assert _code(eng.append, t["batch"], wide[:, :8], t["k"], t["v"], t["pos"], _spec(), t["k_pool"], t["v_pool"],
+                 q_out=wide.view(8, 8, 128)[:4]) == -1
+    from paper_2508_17892_b200.paged import IlrePagedPool
+    pool = IlrePagedPool(t["k_pool"].data_ptr(), t["v_pool"].data_ptr(), t["w_pool"].data_ptr(), 0, 0, b.n_pages)
+    kept = torch.zeros(4, dtype=torch.int32, device="cuda")
+    assert eng._lib.ilre_paged_evict(eng._h, t["batch"].ref, 2 ** 31 - 1, 0, 0, 0, ctypes.byref(pool), None, 0,
+                                     kept.data_ptr(), kept.data_ptr(), None) == -3
+    host = PagedBatch(t["q_start"].cpu(), t["kv_len"].cpu(), t["table"].cpu(), 4, 2)      # arrays on another device
+    with pytest.raises(AssertionError):
+        eng.attention(host, t["q"], t["k_pool"], t["v_pool"])
+    with pytest.raises(AssertionError):
+        eng.append(host, None, t["k"], t["v"], None, None, t["k_pool"], t["v_pool"])
+    with pytest.raises(AssertionError):
+        eng.evict(host, 8, 0, 0, t["k_pool"], t["v_pool"], t["w_pool"])
+    _close(eng)

@@ -78,3 +78,19 @@ def test_the_bindings_constants_are_the_headers():
                                                                           "float16": value["ILRE_F16"]}
     assert paged._SCALINGS == {"none": value["ILRE_ROPE_PLAIN"], "linear": value["ILRE_ROPE_LINEAR"],
                                "banded": value["ILRE_ROPE_BANDED"], "yarn": value["ILRE_ROPE_YARN"]}
+
+
+def test_rope_in_place_needs_one_stride(lib):
+    from paper_2508_17892_b200.paged import IlreRopeSpec
+    spec = IlreRopeSpec(10000.0, 64, 0, 0, 1.0, 0.0, 0.0, 0.0, 0.0)
+    call = lambda xs, os_: lib.ilre_rope(ctypes.byref(spec), 4096, xs, 4096, os_, 4096, 4, 2, 128, 0, 0, None)  # noqa: E731
+    assert call(256, 512) == -1 and call(512, 256) == -1
+
+
+def test_rope_specs_are_copied_and_pickled():
+    import copy
+    import pickle
+    from paper_2508_17892_b200 import RopeSpec
+    a = RopeSpec(theta=10000.0, rotary_dim=64, interleaved=True, scaling="yarn", factor=4.0, low=1.0, high=32.0)
+    for b in (copy.copy(a), copy.deepcopy(a), pickle.loads(pickle.dumps(a))):
+        assert b == a and bytes(b._c) == bytes(a._c) and b.ref is not a.ref
