@@ -11,6 +11,16 @@
 
 namespace ilre {
 
+// Zeros below the lowest set bit of x > 0, at most `most`.
+__host__ __device__ inline int low_zeros(int x, int most) {
+#ifdef __CUDA_ARCH__
+  const int z = __ffs(x) - 1;
+#else
+  const int z = __builtin_ctz(static_cast<unsigned>(x));
+#endif
+  return z < most ? z : most;
+}
+
 // One head of one sequence: n query tokens in tiles of `tq`, the last of them seeing all kv rows, keys in tiles
 // of 2^tk_shift.  Every query tile has at least one key tile (a tile that sees nothing still writes its output).
 // Lengths stay below 2^31 - 2048, so what a tile sees fits 32 bits; sums take 64.
@@ -26,28 +36,26 @@ struct HeadTiles {
     return seen <= 0 ? 1 : static_cast<int>((static_cast<unsigned>(seen) + (1u << tk_shift) - 1) >> tk_shift);
   }
   // Key tiles of the query tiles before qt <= n_qt() - 1.  Tile i behind those that see nothing counts
-  // f(i) = (b + i tq) >> tk_shift, and f(i + P) = f(i) + s with P a power of two (2 for tq = 64 and 128 keys): k whole
-  // periods and a rest, no division.
+  // f(i) = (b + i tq) >> tk_shift, and with tq = odd 2^z: f(i) = (c + i odd) >> p_shift, c = b >> z.  Over a period of
+  // P = 2^p_shift the remainders are each number below P once, so its sum is c + (odd - 1)(P - 1) / 2, and
+  // f(i + P) = f(i) + odd: k whole periods in closed form and a rest of less than P terms (P is 2 for tq = 64 and 128 keys).
   __host__ __device__ long long before(int qt) const {
+    if (qt == 0) return 0;
     const int pre = kv - n;
-    int blind = pre < 0 ? static_cast<int>(static_cast<unsigned>(-pre) / tq) : 0;        // tiles that see nothing
+    const int blind = pre < 0 ? static_cast<int>(static_cast<unsigned>(-pre) / tq) : 0;  // tiles that see nothing
     if (blind >= qt) return static_cast<long long>(qt) * (1 + extra);
-    const unsigned b = static_cast<unsigned>(pre + (blind + 1) * tq) + (1u << tk_shift) - 1;
-    int z = 0;
-    while (z < tk_shift && !((tq >> z) & 1)) ++z;
-    const int p_shift = tk_shift - z, P = 1 << p_shift, terms = qt - blind;
-    const long long k = terms >> p_shift, s = tq >> z;
-    const int r = terms & (P - 1);
-    long long whole = 0, rest = 0;
-    for (int i = 0; i < (k ? P : r); ++i) {
-      const unsigned f = (b + static_cast<unsigned>(i) * tq) >> tk_shift;
-      whole += f;
-      if (i < r) rest += f;
-    }
-    return blind + k * whole + s * P * (k * (k - 1) / 2) + rest + s * k * r + static_cast<long long>(qt) * extra;
+    const int z = low_zeros(tq, tk_shift), p_shift = tk_shift - z, P = 1 << p_shift, terms = qt - blind;
+    const unsigned c = (static_cast<unsigned>(pre + (blind + 1) * tq) + (1u << tk_shift) - 1) >> z, odd = tq >> z;
+    const int k = terms >> p_shift, r = terms & (P - 1);
+    const long long whole = c + ((odd - 1) * (P - 1) >> 1);
+    unsigned rest = 0;                     // less than 128 numbers below 2^25
+    for (int i = 0; i < r; ++i) rest += (c + i * odd) >> p_shift;
+    return blind + k * whole + static_cast<long long>(odd) * P * (static_cast<long long>(k) * (k - 1) / 2) + rest +
+           static_cast<long long>(odd) * k * r + static_cast<long long>(qt) * extra;
   }
+  __host__ __device__ bool empty() const { return n <= 0; }
   __host__ __device__ long long units() const {
-    if (n <= 0) return 0;
+    if (empty()) return 0;
     const int last = n_qt() - 1;
     return before(last) + key_tiles(last) + extra;
   }
@@ -76,30 +84,26 @@ struct KeyTiles {
   }
   __host__ __device__ int key_tiles(int kt) const { return row_tiles() - first(kt); }
   // Units of the key tiles before kt: all row tiles less those that see none, first(i) = (b + i 2^tk_shift) / tq from
-  // key tile `seen` on, which repeats with a period of tq / gcd.
+  // key tile `seen` on; with tq = P 2^z and s = 2^(tk_shift - z) that is (c + i s) / P, c = b >> z, whose sum over a period
+  // of P tiles is c + (s - 1)(P - 1) / 2 (the remainders are each number below P once; P = 1 where tq is a power of two).
   __host__ __device__ long long before(int kt) const {
+    if (kt == 0) return 0;
     const int pre = kv - n;
     const int seen = pre <= 0 ? 0 : static_cast<int>((static_cast<unsigned>(pre) + (1u << tk_shift) - 1) >> tk_shift);
     const long long all = static_cast<long long>(kt) * (row_tiles() + extra);
     if (seen >= kt) return all;
-    const unsigned b = static_cast<unsigned>((seen << tk_shift) - pre);
-    int z = 0;
-    while (z < tk_shift && !((tq >> z) & 1)) ++z;
-    const int P = tq >> z, s = 1 << (tk_shift - z), terms = kt - seen;
-    if (P == 1)                            // tq a power of two: first(i) = (b >> z) + i s
-      return all - (static_cast<long long>(terms) * (b >> z) + static_cast<long long>(s) * terms * (terms - 1) / 2);
-    const long long k = terms / P;
-    const int r = terms - static_cast<int>(k) * P;
-    long long whole = 0, rest = 0;
-    for (int i = 0; i < (k ? P : r); ++i) {
-      const unsigned f = (b + (static_cast<unsigned>(i) << tk_shift)) / tq;
-      whole += f;
-      if (i < r) rest += f;
-    }
-    return all - (k * whole + static_cast<long long>(s) * P * (k * (k - 1) / 2) + rest + s * k * r);
+    const int z = low_zeros(tq, tk_shift), P = tq >> z, s = 1 << (tk_shift - z), terms = kt - seen;
+    const unsigned c = static_cast<unsigned>((seen << tk_shift) - pre) >> z;
+    const int k = P == 1 ? terms : terms / P, r = terms - k * P;
+    const long long whole = c + ((s - 1) * (P - 1) >> 1);
+    long long rest = 0;
+    for (int i = 0; i < r; ++i) rest += (c + static_cast<unsigned>(i) * s) / P;     // (no term where P = 1)
+    return all - (k * whole + static_cast<long long>(s) * P * (static_cast<long long>(k) * (k - 1) / 2) + rest +
+                  static_cast<long long>(s) * k * r);
   }
+  __host__ __device__ bool empty() const { return n <= 0 || kv <= 0; }
   __host__ __device__ long long units() const {
-    if (n <= 0 || kv <= 0) return 0;
+    if (empty()) return 0;
     const int last = n_qt() - 1;
     return before(last) + key_tiles(last) + extra;
   }
@@ -187,10 +191,12 @@ struct TileShape {
 };
 
 template <class Tiles>
+__host__ __device__ __forceinline__ long long head_units(const PagedBatch& b, const TileShape& ts, const SeqSpan& s) {
+  return in_range(b, s.n) ? Tiles{s.n, s.kv, ts.tq, ts.tk_shift, ts.extra}.units() : 0;
+}
+template <class Tiles>
 __host__ __device__ __forceinline__ long long seq_units(const PagedBatch& b, const TileShape& ts, int i) {
-  const SeqSpan s = load_span(b, i);
-  if (!in_range(b, s.n)) return 0;
-  return Tiles{s.n, s.kv, ts.tq, ts.tk_shift, ts.extra}.units() * ts.heads;
+  return head_units<Tiles>(b, ts, load_span(b, i)) * ts.heads;
 }
 
 // The query tile of one head that a unit lies in.
@@ -198,6 +204,7 @@ struct Item {
   SeqSpan span;
   int seq, head, qt, n_tiles;              // n_tiles: key tiles
   long long begin;                         // its first unit
+  int n_qt;                                // query tiles of the head
   __host__ __device__ long long tiles_at(const TileShape& ts) const { return begin + ts.extra; }
   __host__ __device__ long long end(const TileShape& ts) const { return begin + ts.extra + n_tiles; }
 };
@@ -226,22 +233,30 @@ __host__ __device__ __forceinline__ int find_tile(const Tiles& t, long long u, l
 #endif
 }
 
-// The item of unit `at` of the sequence `seq` of `units` units, the first of which is seq_begin.
+// The item of unit `at` of the sequence `seq` of `per_head` units a head, the first of which is seq_begin.
 template <class Tiles>
-__host__ __device__ __forceinline__ Item locate(const TileShape& ts, int seq, const SeqSpan& span, long long units,
-                                                long long seq_begin, long long at) {
+__host__ __device__ __forceinline__ Item locate_by_head(const TileShape& ts, int seq, const SeqSpan& span,
+                                                        long long per_head, long long seq_begin, long long at) {
   Item x;
   x.seq = seq;
   x.span = span;
   const Tiles tiles{span.n, span.kv, ts.tq, ts.tk_shift, ts.extra};
-  const long long per_head = div_pos(units, ts.heads), off = at - seq_begin;
+  const long long off = at - seq_begin;
   x.head = static_cast<int>(div_pos(off, per_head));
   const long long in_head = off - x.head * per_head;
   long long before;
   x.qt = find_tile(tiles, in_head, &before);
   x.begin = at - in_head + before;
   x.n_tiles = tiles.key_tiles(x.qt);
+  x.n_qt = tiles.n_qt();
   return x;
+}
+
+// The same of a sequence of `units` units.
+template <class Tiles>
+__host__ __device__ __forceinline__ Item locate(const TileShape& ts, int seq, const SeqSpan& span, long long units,
+                                                long long seq_begin, long long at) {
+  return locate_by_head<Tiles>(ts, seq, span, div_pos(units, ts.heads), seq_begin, at);
 }
 
 struct PlanStart {
@@ -280,7 +295,7 @@ struct PieceWalk {
   // The item from unit `at` on; false if the share has none of its tiles.
   __host__ __device__ __forceinline__ bool open(const TileShape& ts, const Item& x, long long at) {
     p.span = x.span; p.seq = x.seq; p.head = x.head; p.qt = x.qt; p.n_tiles = x.n_tiles; p.item = x.begin;
-    n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.n_qt();
+    n_qt = x.n_qt;
     return close(ts, at);
   }
   __host__ __device__ __forceinline__ bool close(const TileShape& ts, long long at) {
@@ -306,7 +321,7 @@ struct PieceWalk {
           do {                             // units are left, so a sequence with work follows
             if (++p.seq >= b.n_seqs) return false;
             p.span = load_span(b, p.seq);
-          } while (!in_range(b, p.span.n) || Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.units() == 0);
+          } while (!in_range(b, p.span.n) || Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.empty());
           n_qt = Tiles{p.span.n, p.span.kv, ts.tq, ts.tk_shift, ts.extra}.n_qt();
         }
       }

@@ -83,6 +83,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       mbar_init(smem_u32(&tail->o_full[x]), 1);
     }
     fence_mbar_init();
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(&tail->tmem_base), 512);

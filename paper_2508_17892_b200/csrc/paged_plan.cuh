@@ -53,7 +53,8 @@ __device__ __forceinline__ void plan_find(const PagedBatch& b, const TileShape& 
   }
   if (warp < 2) {
     const int seq = static_cast<int>(found[2 * warp]);
-    const Item x = locate<Tiles>(ts, seq, load_span(b, seq), seq_units<Tiles>(b, ts, seq), found[2 * warp + 1], warp ? u1 - 1 : u0);
+    const SeqSpan span = load_span(b, seq);
+    const Item x = locate_by_head<Tiles>(ts, seq, span, head_units<Tiles>(b, ts, span), found[2 * warp + 1], warp ? u1 - 1 : u0);
     if (lane == 0) { if (warp) out->last = x; else out->first = x; }
   }
 }
@@ -64,11 +65,12 @@ __device__ __forceinline__ void plan_small(const PagedBatch& b, const TileShape&
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (warp >= 2) return;
   SeqSpan span = {0, 0, 0};
-  long long n = 0;
+  long long per_head = 0;
   if (lane < b.n_seqs) {
     span = load_span(b, lane);
-    if (in_range(b, span.n)) n = Tiles{span.n, span.kv, ts.tq, ts.tk_shift, ts.extra}.units() * ts.heads;
+    per_head = head_units<Tiles>(b, ts, span);
   }
+  const long long n = per_head * ts.heads;
   long long incl = n;
   for (int o = 1; o < 32 && o < b.n_seqs; o <<= 1) {
     const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
@@ -83,7 +85,7 @@ __device__ __forceinline__ void plan_small(const PagedBatch& b, const TileShape&
   const long long at = warp ? u1 - 1 : u0, begin = incl - n;
   const int seq = __ffs(__ballot_sync(0xFFFFFFFFu, begin <= at && at < incl)) - 1;
   span = SeqSpan{__shfl_sync(0xFFFFFFFFu, span.q0, seq), __shfl_sync(0xFFFFFFFFu, span.n, seq), __shfl_sync(0xFFFFFFFFu, span.kv, seq)};
-  const Item x = locate<Tiles>(ts, seq, span, __shfl_sync(0xFFFFFFFFu, n, seq), __shfl_sync(0xFFFFFFFFu, begin, seq), at);
+  const Item x = locate_by_head<Tiles>(ts, seq, span, __shfl_sync(0xFFFFFFFFu, per_head, seq), __shfl_sync(0xFFFFFFFFu, begin, seq), at);
   if (lane == 0) { if (warp) out->last = x; else out->first = x; }
 }
 

@@ -65,6 +65,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       mbar_init(smem_u32(&tail->empty[s]), kWarps);
     }
     fence_mbar_init();
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
   }
   __syncthreads();
   grid_dep_wait();

@@ -119,6 +119,8 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     for (int s = 0; s < kAccs; ++s) { mbar_init(smem_u32(&tail->d_full[s]), 1); mbar_init(smem_u32(&tail->d_empty[s]), 4); }
     for (int h = 0; h < 2; ++h) { mbar_init(smem_u32(&tail->sums_full[h]), 4); mbar_init(smem_u32(&tail->sums_empty[h]), 4); }
     fence_mbar_init();
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
   }
   // rows that no load brings: zeros, for good
   for (int i = threadIdx.x; i < row_slots * 2 * (n_cols - tile_rows) * 8; i += kThreads) {

@@ -46,6 +46,7 @@ paged_weight_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
       mbar_init(smem_u32(&tail->empty[s]), kWarps);
     }
     fence_mbar_init();
+    tma_prefetch_desc(&map_k);
   }
   __syncthreads();
   grid_dep_wait();
