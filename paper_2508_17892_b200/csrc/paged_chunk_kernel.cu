@@ -508,12 +508,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 }
 
 // Joins the pieces of the item that begins in share blockIdx.x and goes on behind it, if there is one: 32 of its rows
-// (lane = row), a warp per 8 channels.  Bound by latency, so the contributors' statistics are fetched side by side
-// and their outputs eight at a time.  Contributor c's slot is 1 if the item begins in its share, else 0.
-constexpr int kJoinRows = 32, kJoinThreads = 512, kJoinFlight = 8, kMaxCtas = 192;
+// (lane = row), a warp per 8 channels.  Bound by latency, so the contributors' statistics are fetched side by side.
+// Most items have two or three contributors: two outputs of a thread in flight and three CTAs per SM serve them better
+// than eight and one (a ragged batch of 12 sequences 115 -> 107 us in all, 4096 tokens alone 143 -> 135; four and two
+// 108 and 137).  Contributor c's slot is 1 if the item begins in its share, else 0.
+constexpr int kJoinRows = 32, kJoinThreads = 512, kJoinFlight = 2, kMaxCtas = 192;
 
 template <bool kF16>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 3)
 paged_join_kernel(const __grid_constant__ PagedAttnParams p, int tok) {
   __shared__ float2 ml[kMaxCtas][kJoinRows];
   grid_dep_wait();
