@@ -3,9 +3,10 @@
 //
 // Selection: one cluster of CTAs per list (a kv head of a sequence, or a sequence).  Each CTA reads its part of the
 // list's weights once, as numbers that order like them, and keeps them in shared memory; three histograms (11, 11
-// and 10 bits, added up over the cluster through its shared memory) narrow the threshold down, and prefix counts
-// give every row above it, and the first rows equal to it, its place in the ascending output.  Bound by latency: a
-// list is some 10^4 numbers, so what counts is that they are read once and that few barriers follow.
+// and 10 bits, added up over the cluster through its shared memory) narrow the threshold down until its bin
+// is kept as a whole (one request of 4608 rows 13.8 us in all; 15.1 with all three always), and prefix counts give
+// every row above it, and the first rows equal to it, its place in the ascending output.  Bound by latency: a list is
+// some 10^4 numbers, so what counts is that they are read once and that few barriers follow.
 //
 // Moving, to other pages: every row is its own, so CTAs of 64 rows of a head copy them all at once.  In place:
 // the kept rows ascend, so kept row i comes from a row >= i, and rows may move as long as none is written before every
@@ -51,7 +52,7 @@ struct SelShared {
   uint32_t hist[3][kSelBins];
   uint32_t warp_sum[kSelThreads / 32];
   uint32_t above, equal;                                 // of this CTA's part
-  uint32_t bin, left;
+  uint32_t bin, left, held;                              // held: rows of the bin
 };
 
 __device__ __forceinline__ uint32_t ld_cluster(const uint32_t* mine, uint32_t rank) {
@@ -130,6 +131,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
     }
   }
   uint32_t left = want, prefix = 0;                      // rows to take among those whose leading bits are `prefix`
+  int low = 0;                                           // bits behind the prefix
 #pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : kSelBins;
@@ -153,19 +155,21 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
     const uint32_t in_bin[4] = {c.w, c.z, c.y, c.x};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (before < left && left <= before + in_bin[j]) { s.bin = b0 + 3 - j; s.left = left - before; }
+      if (before < left && left <= before + in_bin[j]) { s.bin = b0 + 3 - j; s.left = left - before; s.held = in_bin[j]; }
       before += in_bin[j];
     }
     __syncthreads();
     left = s.left;
     prefix = pass == 0 ? s.bin : pass == 1 ? (prefix << 11) | s.bin : (prefix << 10) | s.bin;
+    low = shift;
+    if (left == s.held) break;                           // the whole bin is kept: its rows need no order
     __syncthreads();
   }
-  // `prefix` is the threshold, `left` the rows equal to it that are kept.  Each thread a run of consecutive rows.
+  // `prefix` is the threshold, `left` the rows equal to it (but for the low bits) that are kept.  Each thread a run of consecutive rows.
   const int run = (n + kSelThreads - 1) / kSelThreads, i0 = min(static_cast<int>(threadIdx.x) * run, n), i1 = min(i0 + run, n);
   uint32_t above = 0, equal = 0;
   for (int i = i0; i < i1; ++i) {
-    const uint32_t k = key_at(i);
+    const uint32_t k = key_at(i) >> low;
     above += k > prefix;
     equal += k == prefix;
   }
@@ -178,7 +182,7 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
   e = __reduce_add_sync(0xFFFFFFFFu, e) + equal_before;
   cluster_sync_all();                                    // no CTA leaves while its counts are read
   for (int i = i0; i < i1; ++i) {
-    const uint32_t k = key_at(i);
+    const uint32_t k = key_at(i) >> low;
     const bool is_above = k > prefix, is_equal = k == prefix;
     if (is_above || (is_equal && e < left)) kept[p.n_sink + a + min(e, left)] = lo + i;
     a += is_above;
@@ -342,8 +346,8 @@ cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st) {
   const int lists = p.per_head ? p.n_kv : 1;
   const long long rows = static_cast<long long>(p.batch.max_blocks) << p.batch.page_shift;
   // Few CTAs for short lists: what a CTA reads of the others' histograms grows with their number (24 KB each, the
-  // longest step: one request of 4608 rows, eight lists, 18.9 us with 8 CTAs, 15.0 with 2; 16 lists of 6000 to 14000
-  // rows 115 with 8, 108 with 4).
+  // longest step: one request of 4608 rows, eight lists, with all three 18.9 us with 8 CTAs, 15.0 with 2, then 13.8 with
+  // 2, 16.0 with 1; 16 lists of 6000 to 14000 rows 115 with 8, 108 with 4).
   const int n_cta = rows <= 8192 ? 2 : rows <= 16384 ? 4 : kSelCluster;
   const long long part = (rows + n_cta - 1) / n_cta;
   const int keep = static_cast<int>(part < kSelKeep ? (part + 3) & ~3ll : kSelKeep);
