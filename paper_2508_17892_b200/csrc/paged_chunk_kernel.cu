@@ -29,8 +29,8 @@ constexpr int kHalf = kTileBytes / 2;                    // 128 rows x 64 channe
 constexpr int kThreads = 352;                            // warp 0 loads, 1 S MMAs, 2 PV MMAs, 3..6 / 7..10 softmax
 constexpr int kSoftmaxWarps = 4;
 constexpr int kEarly = 2;                                // of a tile's four groups, those before the wait for P
-// What an item costs beside its tiles, in tiles.  Ragged batch of 12 sequences, 4096 tokens alone: 0 148 / 211 us, 2
-// 119 / 176, 3 113 / 173, 4 116 / 176.
+// What an item costs beside its tiles, in tiles.  Ragged batch of 12 sequences, 4096 tokens alone: 0 136 / 180 us, 2
+// 108 / 135, 3 107 / 135, 4 110 / 138.
 constexpr int kItemUnits = 3;
 constexpr int kMinUnits = 4;                             // that a CTA gets at least (64 tokens behind 4096 rows: 2 25.8 us, 4 24.9)
 
