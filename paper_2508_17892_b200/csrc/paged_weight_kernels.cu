@@ -308,7 +308,9 @@ paged_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         // column c is row (token c / group, head c % group) of the tile: seen from column lo on, rows up to hi
         const int tok0 = (job.row_tile + u) * ts.tq;
         const int hi = min(ts.tq, job.n - tok0) * p.group;
-        const int lo = (key - pre - tok0) * p.group;
+        // (clamped first: 32 heads times the distance of a row 67 million back would pass 32 bits.  Above, the distance
+        // stays below a key tile and a row tile, since the unit sees some of the keys)
+        const int lo = max(key - pre - tok0, 0) * p.group;
         const bool masked = hi < tile_rows || job.kt * 256 + half * 128 + 127 > pre + tok0;
         const uint32_t d = lane_base + acc * kCols;
         // (not unrolled: the code stays in the instruction cache, the other groups cover the waits)
