@@ -14,6 +14,16 @@ static constexpr int kRowKeys = 64;              // keys of a stage
 static constexpr int kRowCtasPerSm = 2;
 static constexpr int kChunkRows = 256;           // query rows of a work item of the chunk kernel
 
+// The probabilities are rounded to the cache's type for their product with the values, which the tensor cores take no
+// other way at this rate: half a step each (bf16 2^-8, fp16 2^-11), as the output; their sum is of the unrounded ones.
+// Against 64 bits the output's error is 1.4 times the 32-bit form's (bf16 0.0023 against 0.0017 of its norm).
+// fp16 ends at 2^-24, and in a long cache most of a row's weight may lie in probabilities below that times the largest
+// (2^17 of 2^-26 each came out as nothing), so there they are held 2^kRowShift or 2^kChunkShift times as large, sum and output
+// alike: the quotient does not change, and the logarithm takes it off again.  The largest is then 2^15.
+static constexpr float kRowShift = 15.f;         // the row kernel's reference is the maximum itself
+static constexpr float kChunkSlack = 8.f;        // the chunk kernel's may lag behind it by 2^8: the output is rescaled less often
+static constexpr float kChunkShift = 7.f;
+
 // The cut item that begins in a CTA's share: its last CTA (-1: there is none), first token, tokens, kv head.
 struct ChunkJoin {
   int c_last, token, n_tok, head;

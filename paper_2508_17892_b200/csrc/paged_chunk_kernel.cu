@@ -310,7 +310,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       if (tok0 < walk->p.span.n) {
         const int pre = kv - walk->p.span.n + tok0;      // what its first token sees
         const int limit = pre + my_tok;
-        constexpr float kRefSlack = 8.f;                 // log2 units
+        constexpr float kShift = kF16 ? kChunkShift : 0.f;
         float ref = -INFINITY, l = 0.f;
         for (int i = 0; i < n && ok; ++i, ++n_tile) {
           ok = warp_wait(&tail->s_full[x], n_tile & 1u, abort_flag, b.status, kDevWaitAccFull);
@@ -339,11 +339,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           }
           const float cm = fmax3(m0, m1, fmaxf(V(126), V(127)));
           float scale = 1.f;
-          if ((cm - ref) * c2 > kRefSlack || ref == -INFINITY) {
+          if ((cm - ref) * c2 > kChunkSlack || ref == -INFINITY) {
             scale = (ref == -INFINITY) ? 0.f : ex2_approx((ref - cm) * c2);
             ref = (cm == -INFINITY) ? ref : cm;
           }
-          const float nr = (ref == -INFINITY) ? 0.f : -ref * c2;
+          const float nr = (ref == -INFINITY) ? 0.f : fmaf(-ref, c2, kShift);
           float2 sum2 = make_float2(0.f, 0.f);
           auto exponentials = [&](int g32, uint32_t (&wd)[16]) {
 #pragma unroll
@@ -464,7 +464,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             __syncwarp();
             if (p.lse && my_tok < valid_tok)
               p.lse[(tok_at + my_tok) * p.n_q + head0 + my_head] =
-                  l == 0.f ? -INFINITY : (ref * c2 + log2f(l)) * 0.69314718f;
+                  l == 0.f ? -INFINITY : (ref * c2 + (log2f(l) - kShift)) * 0.69314718f;
           } else {
             // partial: [channel / 4][row][4], so that the lanes' stores join
             const long long slot = blockIdx.x * 2 + (walk->p.t0 > 0 ? 0 : 1);
@@ -560,7 +560,7 @@ paged_join_kernel(const __grid_constant__ PagedAttnParams p, int tok) {
   reinterpret_cast<uint4*>(p.out)[at * 16 + warp] =
       make_uint4(pack2<kF16>(a.x * inv, a.y * inv), pack2<kF16>(a.z * inv, a.w * inv), pack2<kF16>(b.x * inv, b.y * inv),
                  pack2<kF16>(b.z * inv, b.w * inv));
-  if (p.lse && warp == 0) p.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718f;
+  if (p.lse && warp == 0) p.lse[at] = L == 0.f ? -INFINITY : (M + (log2f(L) - (kF16 ? kChunkShift : 0.f))) * 0.69314718f;
 }
 
 }  // namespace

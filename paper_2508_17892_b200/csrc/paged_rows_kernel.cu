@@ -57,6 +57,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   volatile int* abort_flag = &tail->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PagedBatch& b = p.batch;
+  constexpr float kShift = kF16 ? kRowShift : 0.f;
 
   if (threadIdx.x == 0) {
     tail->abort_flag = tail->issued = 0;
@@ -195,7 +196,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             m0 = n0; m1 = n1;
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { x0[i] = ex2_approx(x0[i] - z0); x1[i] = ex2_approx(x1[i] - z1); }
+          for (int i = 0; i < 4; ++i) {                    // (the shift behind the difference: it is 0 at most, exactly)
+            x0[i] = ex2_approx(kF16 ? (x0[i] - z0) + kShift : x0[i] - z0);
+            x1[i] = ex2_approx(kF16 ? (x1[i] - z1) + kShift : x1[i] - z1);
+          }
           l0 += (x0[0] + x0[1]) + (x0[2] + x0[3]);
           l1 += (x1[0] + x1[1]) + (x1[2] + x1[3]);
           const uint32_t pa[4] = {pack2<kF16>(x0[0], x0[1]), pack2<kF16>(x1[0], x1[1]), pack2<kF16>(x0[2], x0[3]),
@@ -271,7 +275,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
             for (int j = 0; j < 16; ++j)
               dst[j * 4 + (c0 >> 1)] = x ? pack2<kF16>(o[j][2] * i1, o[j][3] * i1) : pack2<kF16>(o[j][0] * i0, o[j][1] * i0);
-            if (p.lse && (lane & 3) == 0) p.lse[at] = x ? (M1 + log2f(L1)) * 0.69314718f : (M0 + log2f(L0)) * 0.69314718f;
+            if (p.lse && (lane & 3) == 0) p.lse[at] = (x ? M1 + (log2f(L1) - kShift) : M0 + (log2f(L0) - kShift)) * 0.69314718f;
           }
         } else {
           float* po = p.part_o + static_cast<long long>(slot) * kMergeFloats;
@@ -339,7 +343,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const long long at = row_elem(r) * p.n_q + h_first + r % rs.hs;
             uint2* dst = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * 128) + lane;
             *dst = make_uint2(pack2<kF16>(acc.x * inv, acc.y * inv), pack2<kF16>(acc.z * inv, acc.w * inv));
-            if (p.lse && lane == 0) p.lse[at] = (M + log2f(L)) * 0.69314718f;
+            if (p.lse && lane == 0) p.lse[at] = (M + (log2f(L) - kShift)) * 0.69314718f;
           }
         }
         sync_consumers();                                  // tail->last is written again by the next piece

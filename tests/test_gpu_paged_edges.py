@@ -1,0 +1,49 @@
+"""Edges of the paged-cache operators: probabilities far below the largest, sequences and pages that are left out, lists
+longer than the selection's shared memory."""
+import pytest
+import torch
+
+import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, FP = torch.bfloat16, torch.float16
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n_new", [1, 40])
+def test_many_small_probabilities_beside_large_ones(n_new, dtype):
+    """Four rows' logits are 26 powers of two above those of 2^17 others, whose values are 1 while theirs are 0: the output
+    is what the small probabilities sum up to, 2^-11.  As many sequences as keep a CTA on each, so that the large ones are
+    its maximum from the first tile on (one in each run of 16 keys)."""
+    from paper_2508_17892_b200 import PagedCache
+    page, kv, n_seqs = 1024, 1 << 17, 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    eng = PagedCache(n_kv_heads=1, n_q_heads=1, page_size=page, dtype=dtype, max_seqs=n_seqs)
+    k_pool = torch.zeros(2, page, 1, 128, dtype=dtype, device="cuda")
+    v_pool = torch.ones_like(k_pool)
+    for row in (3, 19, 35, 51):
+        k_pool[0, row, 0, 0], v_pool[0, row] = 12.75, 0.0
+    table = torch.ones(n_seqs, kv // page, dtype=torch.int32, device="cuda")   # all rows but the first page's are one page's
+    table[:, 0] = 0
+    q_start = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda") * n_new
+    batch = eng.batch(q_start, torch.full((n_seqs,), kv, dtype=torch.int32, device="cuda"), table, n_seqs * n_new, n_new)
+    q = torch.zeros(n_seqs * n_new, 1, 128, dtype=dtype, device="cuda")
+    q[:, :, 0] = 16.0
+    out, lse = eng.attention(batch, q, k_pool, v_pool, want_lse=True)
+    eng.check_status()
+    top = 16.0 * 12.75 / 128 ** 0.5
+    small = torch.exp(torch.tensor(-top, dtype=torch.float64))
+    rows = torch.arange(kv - n_new - 3, kv - 3, dtype=torch.float64).repeat(n_seqs)      # small ones that each token sees
+    total = 4 + rows * small
+    want = (rows * small / total)[:, None]
+    # fp16: a probability is rounded at 2^7 times its ratio to the largest one (2^15 where a group's rows are few), so each
+    # is off by at most 2^-25-7 of the largest, for 2^17 values of 1; bf16: by half a step of itself.  A thread adds to its
+    # sums once per tile of 64 or 128 keys, at most 2^11 times; each addition to a sum between 1 and 2 may lose 2^-24 (the small
+    # terms beside a large one do), so a sum is off by at most 2^-13 of itself, numerator and denominator both, and lse
+    # by as much and 2^-16 for the logit 18.03 and the logarithm.  The output is rounded by half a step.
+    u = ref.half_step(dtype)
+    tol = want * (2 * u + 2.0 ** -12) + (kv * 2.0 ** -32 / 4 if dtype == FP else 0.0)
+    err = (out[:, 0].double().cpu() - want).abs()
+    assert bool((err <= tol).all()), (float(err.max()), float(tol.min()))
+    assert float((lse[:, 0].double().cpu() - (top + torch.log(total))).abs().max()) <= 2.0 ** -13 + 2.0 ** -16
+    eng.close()
