@@ -521,7 +521,8 @@ int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, cons
  * [n_seqs][dst_blocks] (dst_blocks * page_size >= budget; disjoint from the pages of the batch).  Weights are >= 0
  * (NaN counts as the largest, zeros of either sign as equal; lower ones rank below).
  *   kept_out_dev     int32 [n_seqs][per_head ? n_kv_heads : 1][budget]: kept rows ascending, then -1
- *   new_len_out_dev  int32 [n_seqs]: min(kv_len, budget); may be kv_len_dev itself
+ *   new_len_out_dev  int32 [n_seqs]: min(kv_len, budget), 0 for a sequence that is left out; may be
+ *                    kv_len_dev itself (there a sequence that is left out keeps its entry)
  * q_start_dev is not read (may be NULL).  n_sink + n_recent <= budget (ILRE_ERR_BUDGET)
  * < 2^31 - 4097 (ILRE_ERR_CAPACITY).
  */

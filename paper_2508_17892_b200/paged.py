@@ -296,7 +296,7 @@ class PagedCache:
         """Cuts every sequence to ``budget`` rows: its first n_sink, its last n_recent and the heaviest between them,
         moved to rows 0, 1, ... of its own pages or of dst_table's (int32 [n_seqs, dst_blocks]).  Returns (kept
         int32 [n_seqs, n_kv_heads or 1, budget], ascending, -1 behind a shorter sequence; new_len int32 [n_seqs],
-        which may be batch.kv_len)."""
+        0 where a sequence's length was out of range; it may be batch.kv_len, which keeps such an entry)."""
         if stream is not None:
             with _on_stream(stream, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len, batch.block_table)):
                 return self.evict(batch, budget, n_sink, n_recent, k_pool, v_pool, w_pool, per_head, dst_table, kept, new_len)

@@ -47,3 +47,22 @@ def test_many_small_probabilities_beside_large_ones(n_new, dtype):
     assert bool((err <= tol).all()), (float(err.max()), float(tol.min()))
     assert float((lse[:, 0].double().cpu() - (top + torch.log(total))).abs().max()) <= 2.0 ** -13 + 2.0 ** -16
     eng.close()
+
+
+def test_eviction_gives_a_length_to_sequences_left_out():
+    """A sequence whose length is out of range has 0 rows in new_len, unless that is the batch's own array."""
+    from paper_2508_17892_b200 import PagedCache
+    b = ref.Batch([0, 0, 0], [40, 50, 60], 16, 2, 8, seed=2, spare=8)
+    for bad in (-1, 10 ** 6):
+        for in_place in (True, False):
+            eng = PagedCache(n_kv_heads=2, n_q_heads=8, page_size=16, max_seqs=3)
+            t = b.gpu(eng)
+            t["kv_len"][1] = bad
+            dst = None if in_place else torch.tensor(b.free[:6], dtype=torch.int32).view(3, 2)[:, :1].contiguous().cuda()
+            for own in (False, True):
+                new_len = t["kv_len"] if own else torch.full((3,), 7, dtype=torch.int32, device="cuda")
+                kept, n = eng.evict(t["batch"], 8, 0, 0, t["k_pool"].clone(), t["v_pool"].clone(), t["w_pool"].clone(),
+                                    new_len=new_len, dst_table=dst)
+                assert eng.status() == -10
+                assert n.tolist() == [8, bad if own else 0, 8] and bool((kept[1] == -1).all())
+            eng.close()
