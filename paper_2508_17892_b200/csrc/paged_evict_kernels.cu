@@ -33,7 +33,7 @@ constexpr int kMoveCols = 8;                             // columns of a head: 4
 // not hang on an order.
 __device__ __forceinline__ uint32_t weight_key(const EvictParams& p, int list, int t, int entry) {
   const int page = checked_page(p.batch, entry);
-  if (page >= p.batch.n_pages) return 0;
+  if (page >= p.batch.n_pages) return float_to_ordered(0.f);      // its rows' weights count as zeros
   const int row = t & ((1 << p.batch.page_shift) - 1);
   const float* w = p.w + ((static_cast<long long>(page) * p.n_kv) << p.batch.page_shift) + row;
   float x;

@@ -66,3 +66,18 @@ def test_eviction_gives_a_length_to_sequences_left_out():
                 assert eng.status() == -10
                 assert n.tolist() == [8, bad if own else 0, 8] and bool((kept[1] == -1).all())
             eng.close()
+
+
+@pytest.mark.parametrize("per_head", [True, False])
+def test_eviction_weighs_rows_of_missing_pages_as_zeros(per_head):
+    """All weights are 0 and so are those of a page out of range: the lower rows stay, whichever page they lie in."""
+    from paper_2508_17892_b200 import PagedCache
+    b = ref.Batch([0], [64], 16, 1, 1, seed=3)
+    b.w_pool.zero_()
+    eng = PagedCache(n_kv_heads=1, n_q_heads=1, page_size=16, max_seqs=1)
+    t = b.gpu(eng)
+    t["table"][0, 1] = b.n_pages
+    kept, n = eng.evict(t["batch"], 40, 0, 0, t["k_pool"], t["v_pool"], t["w_pool"], per_head=per_head)
+    assert eng.status() == -10
+    assert n.tolist() == [40] and kept.flatten().tolist() == list(range(40))
+    eng.close()
