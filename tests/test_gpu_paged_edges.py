@@ -81,3 +81,34 @@ def test_eviction_weighs_rows_of_missing_pages_as_zeros(per_head):
     assert eng.status() == -10
     assert n.tolist() == [40] and kept.flatten().tolist() == list(range(40))
     eng.close()
+
+
+def test_eviction_of_a_list_that_shared_memory_does_not_hold():
+    """400000 rows: each of the eight CTAs of the list keeps 44032 keys, the others are read again in every pass.  Few
+    distinct weights, so that thousands tie at the threshold; then all different."""
+    from paper_2508_17892_b200 import PagedCache
+    page, kv, budget, sink, recent = 1024, 400_000, 150_001, 5, 70
+    blocks = -(-kv // page)
+    g = torch.Generator().manual_seed(6)
+    table = torch.randperm(blocks, generator=g).to(torch.int32)[None]
+    for distinct in (50, 1 << 24):
+        w = torch.randint(0, distinct, (blocks, 1, page), generator=g).float()
+        eng = PagedCache(n_kv_heads=1, n_q_heads=1, page_size=page, max_seqs=1)
+        cu = lambda x: x.cuda()  # noqa: E731
+        t = torch.arange(kv)
+        key = w[table[0, t // page].long(), 0, t % page]
+        mid = torch.sort(key[sink:kv - recent], descending=True, stable=True).indices[:budget - sink - recent] + sink
+        want = torch.cat([torch.arange(sink), mid.sort().values, torch.arange(kv - recent, kv)])
+        pool = torch.randn(blocks, page, 1, 128, generator=g).to(BF)
+        batch = eng.batch(None, torch.tensor([kv], dtype=torch.int32).cuda(), cu(table), 0, 0)
+        for per_head in (True, False):
+            k, v, wg = cu(pool), cu(pool).neg(), cu(w)
+            kept, n = eng.evict(batch, budget, sink, recent, k, v, wg, per_head=per_head)
+            eng.check_status()
+            assert n.tolist() == [budget] and torch.equal(kept.flatten().long().cpu(), want)
+            i = torch.arange(budget)
+            to, row, src, src_row = table[0, i // page].long(), i % page, table[0, want // page].long(), want % page
+            assert torch.equal(k.cpu()[to, row], pool[src, src_row]) and torch.equal(v.cpu()[to, row], -pool[src, src_row])
+            assert torch.equal(wg.cpu()[to, 0, row], w[src, 0, src_row])
+        assert eng.check_guards() == 0
+        eng.close()
