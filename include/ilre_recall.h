@@ -404,7 +404,8 @@ typedef struct {
 /*
  * Rotates x [n_tokens][n_heads][head_dim] (dtype ILRE_BF16 or ILRE_F16; heads contiguous, x_stride
  * elements from token to token) by the tokens' positions pos_dev (int32 [n_tokens], any value) into out
- * (out_stride from token to token; out may be x with the same stride, else they do not overlap).
+ * (out_stride from token to token; out may be x with the same stride, else they do not overlap:
+ * ILRE_ERR_INVALID_ARG where rows of one stride do, or the spans of rows of two strides).
  * transposed != 0 applies the transposed map, which is the gradient's: the angles are negated and
  * attn_factor still multiplies.  head_dim a multiple of 16 up to 1024 (ILRE_ERR_UNSUPPORTED), both
  * pointers 16-byte aligned and both strides multiples of 8 elements (ILRE_ERR_ALIGNMENT), strides at least
@@ -476,7 +477,8 @@ int ilre_paged_create(const ilre_paged_config_t* cfg, ilre_paged_t** out);
  * New tokens into the cache: k [n_tokens][n_kv_heads][128] is rotated by the tokens' positions (ilre_rope)
  * and v copied to the rows of the new tokens, their accumulated weights (w_dev, if given) are set to
  * 0, and q [n_tokens][n_q_heads][128] is rotated into q_out.  Strides in elements from token to token
- * (multiples of 8; q_out may be q with its stride, else they do not overlap).  q_dev and q_out_dev may both
+ * (multiples of 8; q_out may be q with its stride, else they do not overlap, nor q_out and k or v: refused
+ * as in ilre_rope; k and v may lie in the pools, but not in rows that the call writes).  q_dev and q_out_dev may both
  * be NULL, and spec NULL copies without a rotation (pos_dev may then be NULL).  Positions are given apart from
  * the rows because after an eviction they differ.  kv_len[i] >= n_i (else the sequence is left out and
  * reported); rows that are written belong to one sequence, on one page.

@@ -145,9 +145,23 @@ int validate_rows(const void* base, int64_t stride, int64_t heads, int head_dim)
   return ILRE_OK;
 }
 
-// Rows turned in place: every thread writes what it read, so the strides must agree.
-int validate_in_place(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t n) {
-  return in == out && in_stride != out_stride && n > 1 ? ILRE_ERR_INVALID_ARG : ILRE_OK;
+// Do n rows of a (a_row elements, a_stride from one to the next) and n rows of b share memory?  Rows of one stride are told
+// apart even where they alternate (slices of one tensor); with two strides the spans count.
+bool rows_overlap(const void* a, int64_t a_stride, int64_t a_row, const void* b, int64_t b_stride, int64_t b_row, int64_t n) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  if (a0 >= b0 + static_cast<uintptr_t>((n - 1) * b_stride + b_row) * 2 ||
+      b0 >= a0 + static_cast<uintptr_t>((n - 1) * a_stride + a_row) * 2)
+    return false;
+  if (n == 1 || a_stride != b_stride) return true;
+  const int64_t step = a_stride * 2, apart = static_cast<int64_t>(b0 - a0) % step;
+  const int64_t behind = apart < 0 ? apart + step : apart;     // from a row of a to the next one of b
+  return behind < a_row * 2 || behind + b_row * 2 > step;
+}
+
+// Rows turned in place: every thread writes what it read, so the strides must agree; other rows must not be written.
+int validate_in_place(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t row, int64_t n) {
+  if (in == out) return in_stride != out_stride && n > 1 ? ILRE_ERR_INVALID_ARG : ILRE_OK;
+  return rows_overlap(in, in_stride, row, out, out_stride, row, n) ? ILRE_ERR_INVALID_ARG : ILRE_OK;
 }
 
 // Query rows are read by many CTAs while others write their output.
@@ -226,7 +240,7 @@ int ilre_rope(const ilre_rope_spec_t* spec, const void* x_dev, int64_t x_stride,
   if (!aligned4(pos_dev)) return ILRE_ERR_ALIGNMENT;
   ILRE_CHECK(validate_rows(x_dev, x_stride, n_heads, head_dim));
   ILRE_CHECK(validate_rows(out_dev, out_stride, n_heads, head_dim));
-  ILRE_CHECK(validate_in_place(x_dev, x_stride, out_dev, out_stride, n_tokens));
+  ILRE_CHECK(validate_in_place(x_dev, x_stride, out_dev, out_stride, static_cast<int64_t>(n_heads) * head_dim, n_tokens));
   int dev = 0, n_sm = 0;
   ILRE_CUDA(cudaGetDevice(&dev));
   ILRE_CUDA(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
@@ -313,7 +327,11 @@ int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const il
   if (q_dev) {
     ILRE_CHECK(validate_rows(q_dev, q_stride, h->cfg.n_q_heads, kDim));
     ILRE_CHECK(validate_rows(q_out_dev, q_out_stride, h->cfg.n_q_heads, kDim));
-    ILRE_CHECK(validate_in_place(q_dev, q_stride, q_out_dev, q_out_stride, batch->n_tokens));
+    const int64_t q_row = static_cast<int64_t>(h->cfg.n_q_heads) * kDim, kv_row = static_cast<int64_t>(h->cfg.n_kv_heads) * kDim;
+    ILRE_CHECK(validate_in_place(q_dev, q_stride, q_out_dev, q_out_stride, q_row, batch->n_tokens));
+    if (rows_overlap(k_dev, k_stride, kv_row, q_out_dev, q_out_stride, q_row, batch->n_tokens) ||
+        rows_overlap(v_dev, v_stride, kv_row, q_out_dev, q_out_stride, q_row, batch->n_tokens))
+      return ILRE_ERR_INVALID_ARG;
   }
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return ILRE_ERR_CUDA;

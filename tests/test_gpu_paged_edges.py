@@ -10,6 +10,11 @@ pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float16
 
 
+def _engine(b):
+    from paper_2508_17892_b200 import PagedCache
+    return PagedCache(n_kv_heads=b.n_kv, n_q_heads=b.n_q, page_size=b.page, dtype=b.dtype, max_seqs=len(b.q_len))
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("n_new", [1, 40])
 def test_many_small_probabilities_beside_large_ones(n_new, dtype):
@@ -112,3 +117,39 @@ def test_eviction_of_a_list_that_shared_memory_does_not_hold():
             assert torch.equal(wg.cpu()[to, 0, row], w[src, 0, src_row])
         assert eng.check_guards() == 0
         eng.close()
+
+
+def test_append_refuses_rows_that_are_read_and_written():
+    """q_out over some of q's, k's or v's rows is refused before anything is launched; in place in a fused projection, and
+    into the gap between its slices, it is as ever."""
+    from paper_2508_17892_b200 import IlreError, RopeSpec
+    b = ref.Batch([3, 2], [40, 30], 16, 2, 8, seed=7)
+    eng = _engine(b)
+    t = b.gpu(eng)
+    spec = RopeSpec()
+    want = eng.append(t["batch"], t["q"], t["k"], t["v"], t["pos"], spec, t["k_pool"], t["v_pool"])
+    fused = torch.zeros(5, 24, 128, dtype=BF, device="cuda")
+    q, k, v, gap = fused[:, :8], fused[:, 8:10], fused[:, 10:12], fused[:, 14:22]
+
+    def fill():
+        fused.zero_()
+        q.copy_(t["q"]), k.copy_(t["k"]), v.copy_(t["v"])
+
+    flat = torch.zeros(9, 8, 128, dtype=BF, device="cuda")
+    flat[:5] = t["q"]
+    for args in ((fused[:, 1:9], k, v, q), (q, k, v, fused[:, 1:9]), (q, k, v, fused[:, 4:12]), (fused[:, 14:22], k, v, fused[:, 3:11]),
+                 (flat[:5], t["k"], t["v"], flat[1:6]), (flat[1:6], t["k"], t["v"], flat[:5]),
+                 (t["q"], flat.view(36, 2, 128)[:5], t["v"], flat[:5]), (t["q"], t["k"], flat.view(36, 2, 128)[3:8], flat[:5])):
+        with pytest.raises(IlreError) as e:
+            eng.append(t["batch"], *args[:3], t["pos"], spec, t["k_pool"], t["v_pool"], q_out=args[3])
+        assert e.value.code == -1
+    for out in (q, gap):
+        fill()
+        pools = [torch.zeros_like(t["k_pool"]) for _ in range(2)]
+        eng.append(t["batch"], q, k, v, t["pos"], spec, *pools, q_out=out)
+        assert torch.equal(out, want) and torch.equal(k, t["k"]) and torch.equal(v, t["v"])
+        for i in range(2):
+            pg, row = (x[b.kv_len_list[i] - b.q_len[i]:].cuda() for x in b.slots(i))
+            assert torch.equal(pools[0][pg, row], t["k_pool"][pg, row]) and torch.equal(pools[1][pg, row], t["v_pool"][pg, row])
+    eng.check_status()
+    eng.close()
