@@ -105,13 +105,16 @@ def _rows(t: torch.Tensor, index: int, dtype, heads: int, dim: int) -> int:
     """Stride in elements from token to token of a tensor [n, heads, dim] whose tokens are contiguous."""
     n, h, d = t.shape
     st, sh, sd = t.stride()
-    assert h == heads and d == dim and t.dtype == dtype and t.get_device() == index
-    assert n == 0 or (sd == 1 and (heads == 1 or sh == dim))
+    if not (h == heads and d == dim and t.dtype == dtype and t.get_device() == index):
+        raise AssertionError("rows of another shape, type or device")
+    if n > 0 and (sd != 1 or (heads > 1 and sh != dim)):
+        raise AssertionError("the heads of a token are not contiguous")
     return st if n > 1 else heads * dim
 
 
 def _ints(t: torch.Tensor, index: int, n: int) -> None:
-    assert t.get_device() == index and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous()
+    if not (t.get_device() == index and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous()):
+        raise AssertionError("not a contiguous int32 array of this device and length")
 
 
 def _on_stream(stream: torch.cuda.Stream, tensors):
@@ -137,14 +140,16 @@ def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: b
         with _on_stream(stream, (x, positions, out)):
             return rope(x, positions, spec, transposed, out)
     dtype, index = x.dtype, x.get_device()
-    assert index >= 0 and dtype in _DTYPES
+    if index < 0 or dtype not in _DTYPES:
+        raise AssertionError("x is not a bf16 or fp16 tensor of a CUDA device")
     n, heads, dim = x.shape
     _ints(positions, index, n)
     x_stride = _rows(x, index, dtype, heads, dim)
     if out is None:
         out = torch.empty(n, heads, dim, dtype=dtype, device=x.device)
     out_stride = _rows(out, index, dtype, heads, dim)
-    assert out.shape[0] == n
+    if out.shape[0] != n:
+        raise AssertionError("out has another number of tokens")
     args = (spec.ref, x.data_ptr(), x_stride, out.data_ptr(), out_stride, positions.data_ptr(), n, heads, dim,
             _DTYPES[dtype], int(transposed), _raw_stream(index))
     if torch.cuda.current_device() == index:
@@ -185,31 +190,39 @@ class PagedCache:
         """q_start int32 [n_seqs + 1] (None for ``evict``), kv_len int32 [n_seqs] (the new tokens' rows among
         them), block_table int32 [n_seqs, max_blocks]; at most max_q_len new tokens per sequence."""
         for t in (q_start, kv_len, block_table):
-            assert t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous())
-        assert kv_len.dim() == 1 and block_table.dim() == 2 and block_table.shape[0] == kv_len.numel()
-        assert q_start is None or q_start.shape == (kv_len.numel() + 1,)
+            if not (t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous())):
+                raise AssertionError("the batch's arrays are contiguous int32 tensors of the cache's device")
+        if kv_len.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != kv_len.numel():
+            raise AssertionError("kv_len [n_seqs] and block_table [n_seqs, max_blocks]")
+        if q_start is not None and q_start.shape != (kv_len.numel() + 1,):
+            raise AssertionError("q_start [n_seqs + 1]")
         return PagedBatch(q_start, kv_len, block_table, n_tokens, max_q_len)
 
     def _page_step(self, t: Optional[torch.Tensor], shape) -> int:
         """Stride in elements from page to page (0: back to back)."""
         if t is None:
             return 0
-        assert t.shape == shape and t.dtype == self.dtype and t.get_device() == self._index
+        if not (t.shape == shape and t.dtype == self.dtype and t.get_device() == self._index):
+            raise AssertionError("a pool of another shape, type or device")
         step = t.stride()
-        assert step[1:] == self._page_stride or shape[0] == 0 or t[0].is_contiguous()
+        if not (step[1:] == self._page_stride or shape[0] == 0 or t[0].is_contiguous()):
+            raise AssertionError("a page is not contiguous")
         return step[0] if shape[0] > 1 else 0
 
     def _pool(self, batch: PagedBatch, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
-        assert batch.index == self._index                  # its arrays are read on the handle's device
+        if batch.index != self._index:
+            raise AssertionError("the batch's arrays are on another device")
         n_pages = k.shape[0]
         shape = (n_pages,) + self._page_shape
-        assert w is None or (w.shape == (n_pages,) + self._weight_shape and w.dtype == torch.float32 and
-                             w.is_contiguous() and w.get_device() == self._index)
+        if not (w is None or (w.shape == (n_pages,) + self._weight_shape and w.dtype == torch.float32 and
+                             w.is_contiguous() and w.get_device() == self._index)):
+            raise AssertionError("w_pool of another shape, type or device")
         return IlrePagedPool(k.data_ptr(), _ptr(v), _ptr(w), self._page_step(k, shape), self._page_step(v, shape), n_pages)
 
     def _q(self, batch: PagedBatch, q: torch.Tensor) -> int:
         n = batch.n_tokens
-        assert q.shape[0] == n and (n == 0 or batch.q_start is not None)
+        if not (q.shape[0] == n and (n == 0 or batch.q_start is not None)):
+            raise AssertionError("q has another number of tokens, or the batch no q_start")
         return _rows(q, self._index, self.dtype, self._n_q, self._dim)
 
     def append(self, batch: PagedBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
@@ -223,10 +236,12 @@ class PagedCache:
                                      batch.block_table)):
                 return self.append(batch, q, k, v, positions, spec, k_pool, v_pool, w_pool, q_out)
         n, n_kv, dim = batch.n_tokens, self._page_shape[1], self._dim
-        assert k.shape[0] == n and v.shape[0] == n
+        if k.shape[0] != n or v.shape[0] != n:
+            raise AssertionError("k or v has another number of tokens")
         k_stride = _rows(k, self._index, self.dtype, n_kv, dim)
         v_stride = _rows(v, self._index, self.dtype, n_kv, dim)
-        assert spec is None or positions is not None
+        if spec is not None and positions is None:
+            raise AssertionError("a rotation without positions")
         if positions is not None:
             _ints(positions, self._index, n)
         pool = self._pool(batch, k_pool, v_pool, w_pool)
@@ -237,7 +252,8 @@ class PagedCache:
                 q_out = torch.empty(n, self._n_q, dim, dtype=q.dtype, device=q.device)
             q_out_stride = self._q(batch, q_out)
         else:
-            assert q_out is None
+            if q_out is not None:
+                raise AssertionError("q_out without q")
         rc = self._lib.ilre_paged_append(
             self._h, batch.ref, spec.ref if spec is not None else None, _ptr(positions), _ptr(q), q_stride, _ptr(q_out),
             q_out_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, ctypes.byref(pool), _raw_stream(self._index))
@@ -260,7 +276,8 @@ class PagedCache:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)
         if lse is None and want_lse:
             lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
-        assert out.shape == shape and out.dtype == self.dtype and out.is_contiguous() and out.get_device() == self._index
+        if not (out.shape == shape and out.dtype == self.dtype and out.is_contiguous() and out.get_device() == self._index):
+            raise AssertionError("out is not a contiguous tensor like q")
         self._lse(batch, lse)
         rc = self._lib.ilre_paged_attention(self._h, batch.ref, q.data_ptr(), q_stride, ctypes.byref(pool), out.data_ptr(),
                                             _ptr(lse), _raw_stream(self._index))
@@ -269,8 +286,9 @@ class PagedCache:
         return out, lse
 
     def _lse(self, batch: PagedBatch, lse: Optional[torch.Tensor]) -> None:
-        assert lse is None or (lse.shape == (batch.n_tokens, self._n_q) and lse.dtype == torch.float32 and
-                               lse.is_contiguous() and lse.get_device() == self._index)
+        if not (lse is None or (lse.shape == (batch.n_tokens, self._n_q) and lse.dtype == torch.float32 and
+                               lse.is_contiguous() and lse.get_device() == self._index)):
+            raise AssertionError("lse is not a contiguous fp32 tensor [n_tokens, n_q_heads]")
 
     def accumulate(self, batch: PagedBatch, q: torch.Tensor, lse: torch.Tensor, k_pool: torch.Tensor,
                    w_pool: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
@@ -280,7 +298,8 @@ class PagedCache:
             with _on_stream(stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len, batch.block_table)):
                 return self.accumulate(batch, q, lse, k_pool, w_pool)
         q_stride = self._q(batch, q)
-        assert lse is not None and w_pool is not None
+        if lse is None or w_pool is None:
+            raise AssertionError("lse and w_pool are needed")
         self._lse(batch, lse)
         pool = self._pool(batch, k_pool, None, w_pool)
         rc = self._lib.ilre_paged_accumulate(self._h, batch.ref, q.data_ptr(), q_stride, lse.data_ptr(), ctypes.byref(pool),
@@ -302,17 +321,21 @@ class PagedCache:
                 return self.evict(batch, budget, n_sink, n_recent, k_pool, v_pool, w_pool, per_head, dst_table, kept, new_len)
         n, index = batch.kv_len.numel(), self._index
         shape = (n, self._page_shape[1] if per_head else 1, budget)
-        assert budget >= 1 and w_pool is not None
+        if budget < 1 or w_pool is None:
+            raise AssertionError("a budget of at least 1 and w_pool are needed")
         pool = self._pool(batch, k_pool, v_pool, w_pool)
         dst_blocks = 0
         if dst_table is not None:
-            assert dst_table.get_device() == index and dst_table.dtype == torch.int32 and dst_table.is_contiguous()
-            assert dst_table.dim() == 2 and dst_table.shape[0] == n
+            if not (dst_table.get_device() == index and dst_table.dtype == torch.int32 and dst_table.is_contiguous()):
+                raise AssertionError("dst_table is not a contiguous int32 tensor of the cache's device")
+            if dst_table.dim() != 2 or dst_table.shape[0] != n:
+                raise AssertionError("dst_table [n_seqs, dst_blocks]")
             dst_blocks = dst_table.shape[1]
         if kept is None:
             kept = torch.empty(shape, dtype=torch.int32, device=self.device)
         else:
-            assert kept.shape == shape and kept.dtype == torch.int32 and kept.is_contiguous() and kept.get_device() == index
+            if not (kept.shape == shape and kept.dtype == torch.int32 and kept.is_contiguous() and kept.get_device() == index):
+                raise AssertionError("kept of another shape, type or device")
         if new_len is None:
             new_len = torch.empty(n, dtype=torch.int32, device=self.device)
         else:

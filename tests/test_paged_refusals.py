@@ -47,3 +47,86 @@ def test_rope_refuses_rows_that_are_read_and_written(lib):
             if code != -1:
                 passed.add(code)
     assert passed == {-6}
+
+
+def _optimised(code):
+    """Runs `code` in an interpreter that leaves assert statements out."""
+    r = subprocess.run([sys.executable, "-O", "-c", "import sys\nsys.path.insert(0, %r)\n" % ROOT + code], capture_output=True,
+                       text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-3000:]
+
+
+def test_checks_of_tensors_hold_without_assert_statements(lib):
+    """Under ``python -O`` tensors of another device, type or shape still do not reach the library."""
+    _optimised(r'''
+import torch
+from paper_2508_17892_b200 import paged
+
+class Library:                                               # stands in for the shared object: counts the calls
+    calls = 0
+    def __getattr__(self, name):
+        def call(*a):
+            Library.calls += 1
+            return 0
+        return call
+
+def refused(fn, *a, **kw):
+    try:
+        fn(*a, **kw)
+    except AssertionError:
+        return
+    raise SystemExit("not refused: %s" % (fn,))
+
+paged.load_library = Library
+paged._raw_stream = lambda index: 0
+x, pos = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+refused(paged.rope, x, pos, paged.RopeSpec())                # host tensors
+c = paged.PagedCache.__new__(paged.PagedCache)
+c._lib, c._h, c.dtype, c._n_q, c._dim, c._index, c.device = Library(), None, torch.bfloat16, 8, 128, 0, torch.device("cuda", 0)
+c._page_shape, c._weight_shape, c._page_stride = (16, 2, 128), (2, 16), (256, 128, 1)
+i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+refused(c.batch, i32(3), i32(2), i32(2, 4), 4, 2)
+b = paged.PagedBatch(i32(3), i32(2), i32(2, 4), 4, 2)
+k = torch.zeros(4, 2, 128, dtype=torch.bfloat16)
+pool, w = torch.zeros(3, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 16)
+for index in (0, -1):                                        # the handle's device; then as if the host's tensors were there
+    c._index = index
+    # right shapes pass where the device is the tensors' own
+    if index < 0:
+        c.attention(b, x, pool, pool)
+        c.append(b, x, k, k, pos, None, pool, pool)
+        if Library.calls != 2:
+            raise SystemExit("a call that is right did not reach the library")
+        Library.calls = 0
+    wrong = [x.float(), x[:3], x[:, :4], x.transpose(0, 1)] if index < 0 else [x]
+    for q in wrong:
+        refused(c.attention, b, q, pool, pool)
+        refused(c.append, b, q, k, k, pos, None, pool, pool)
+        refused(c.accumulate, b, q, torch.zeros(4, 8), pool, w)
+    for bad in ([pool.half(), pool[:, :8], pool[:, :, :1]] if index < 0 else [pool]):
+        refused(c.attention, b, x, bad, pool)
+        refused(c.append, b, x, k, k, pos, None, bad, bad)
+        refused(c.evict, b, 8, 0, 0, bad, pool, w)
+    if index < 0:
+        refused(c.attention, b, x, pool, pool, out=x[:2])
+        refused(c.attention, b, x, pool, pool, lse=torch.zeros(4, 7))
+        refused(c.append, b, x, k[:3], k, pos, None, pool, pool)
+        refused(c.append, b, x, k, k, None, paged.RopeSpec(), pool, pool)
+        refused(c.append, b, x, k, k, pos.long(), paged.RopeSpec(), pool, pool)
+        refused(c.append, b, None, k, k, pos, None, pool, pool, q_out=x)
+        refused(c.accumulate, b, x, None, pool, w)
+        refused(c.accumulate, b, x, torch.zeros(4, 8), pool, w.double())
+        refused(c.evict, b, 0, 0, 0, pool, pool, w)
+        refused(c.evict, b, 8, 0, 0, pool, pool, w, dst_table=i32(2, 4).long())
+        refused(c.evict, b, 8, 0, 0, pool, pool, w, kept=i32(2, 1, 7))
+if Library.calls:
+    raise SystemExit("a refused call reached the library")
+''')
+
+
+def test_the_bindings_have_no_assert_statements():
+    import ast
+    import paper_2508_17892_b200 as package
+    for name in ("paged.py",):
+        tree = ast.parse(open(os.path.join(os.path.dirname(package.__file__), name)).read())
+        assert not [n.lineno for n in ast.walk(tree) if isinstance(n, ast.Assert)], name
