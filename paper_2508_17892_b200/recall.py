@@ -118,7 +118,8 @@ def gather_input_ids(input_ids: torch.Tensor, idx: torch.Tensor, query_ids: torc
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Compressed prompt: input_ids at the recalled positions, then the query's ids (int32)."""
     for t in (input_ids, idx, query_ids):
-        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1
+        if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1):
+            raise AssertionError("t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1")
     out = torch.empty(idx.numel() + query_ids.numel(), dtype=torch.int32, device=input_ids.device)
     st = stream if stream is not None else torch.cuda.current_stream(input_ids.device)
     with torch.cuda.device(input_ids.device):
@@ -138,8 +139,10 @@ def layer_recall(idx: torch.Tensor, span_begin: torch.Tensor, span_len: torch.Te
     planted key phrases.  Returns (hits int32 [n_layers, n_spans], phrases retrieved completely
     int32 [n_layers], chosen layer int32 [1]) on the device."""
     for t in (idx, span_begin, span_len):
-        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
-    assert idx.dim() == 2 and span_begin.dim() == 1 and span_begin.shape == span_len.shape
+        if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
+            raise AssertionError("t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()")
+    if not (idx.dim() == 2 and span_begin.dim() == 1 and span_begin.shape == span_len.shape):
+        raise AssertionError("idx.dim() == 2 and span_begin.dim() == 1 and span_begin.shape == span_len.shape")
     n_layers, n_idx = idx.shape
     n_spans = span_begin.numel()
     hits = torch.empty(n_layers, n_spans, dtype=torch.int32, device=idx.device)
@@ -166,7 +169,8 @@ def topk_positions_noalloc(scores: torch.Tensor, k: int,
     on the same device) to keep this wrapper allocation-free too.  ``len(scores)`` must not
     exceed ``NOALLOC_MAX_L``.
     """
-    assert scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()
+    if not (scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()):
+        raise AssertionError("scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()")
     if out_idx is None:
         out_idx = torch.empty(k, dtype=torch.int32, device=scores.device)
     st = stream if stream is not None else torch.cuda.current_stream(scores.device)
@@ -204,11 +208,15 @@ class IlreRecall:
         K: bf16 [L, n_kv_heads, 128] on the device; Q: bf16 [q_len, n_q_heads, 128].
         Returns (indices int32 [n_sink + budget], scores fp32 [L] or None).
         """
-        assert K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16
-        assert K.is_contiguous() and Q.is_contiguous()
+        if not (K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16):
+            raise AssertionError("K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16")
+        if not (K.is_contiguous() and Q.is_contiguous()):
+            raise AssertionError("K.is_contiguous() and Q.is_contiguous()")
         L, q_len = K.shape[0], Q.shape[0]
-        assert K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)
+        if not (K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)):
+            raise AssertionError("K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)")
+        if not (Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)):
+            raise AssertionError("Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)")
         if out_idx is None:
             out_idx = torch.empty(n_sink + budget, dtype=torch.int32, device=K.device)
         if out_scores is None and want_scores:
@@ -225,10 +233,14 @@ class IlreRecall:
 
     # -- key-range sharded recall: the per-rank steps -----------------------------------
     def _check_kq(self, K: torch.Tensor, Q: torch.Tensor):
-        assert K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16
-        assert K.is_contiguous() and Q.is_contiguous()
-        assert K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)
+        if not (K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16):
+            raise AssertionError("K.is_cuda and Q.is_cuda and K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16")
+        if not (K.is_contiguous() and Q.is_contiguous()):
+            raise AssertionError("K.is_contiguous() and Q.is_contiguous()")
+        if not (K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)):
+            raise AssertionError("K.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)")
+        if not (Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)):
+            raise AssertionError("Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)")
 
     def shard_stats(self, K_shard: torch.Tensor, Q: torch.Tensor,
                     out: Optional[torch.Tensor] = None,
@@ -239,8 +251,10 @@ class IlreRecall:
         n_rows = Q.shape[0] * self.cfg.n_q_heads
         if out is None:
             out = torch.empty(n_rows, 2, dtype=torch.float32, device=K_shard.device)
-        assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()
-        assert out.numel() == 2 * n_rows
+        if not (out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()):
+            raise AssertionError("out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()")
+        if not (out.numel() == 2 * n_rows):
+            raise AssertionError("out.numel() == 2 * n_rows")
         st = stream if stream is not None else torch.cuda.current_stream(K_shard.device)
         with torch.cuda.device(K_shard.device):
             rc = self._lib.ilre_recall_shard_stats(self._h, K_shard.data_ptr(), K_shard.shape[0],
@@ -258,12 +272,16 @@ class IlreRecall:
         position order."""
         self._check_kq(K_shard, Q)
         n_rows = Q.shape[0] * self.cfg.n_q_heads
-        assert stats_all.is_cuda and stats_all.dtype == torch.float32 and stats_all.is_contiguous()
-        assert stats_all.dim() == 3 and stats_all.shape[1:] == (n_rows, 2)
+        if not (stats_all.is_cuda and stats_all.dtype == torch.float32 and stats_all.is_contiguous()):
+            raise AssertionError("stats_all.is_cuda and stats_all.dtype == torch.float32 and stats_all.is_contiguous()")
+        if not (stats_all.dim() == 3 and stats_all.shape[1:] == (n_rows, 2)):
+            raise AssertionError("stats_all.dim() == 3 and stats_all.shape[1:] == (n_rows, 2)")
         if out is None:
             out = torch.empty(K_shard.shape[0], dtype=torch.float32, device=K_shard.device)
-        assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()
-        assert out.numel() == K_shard.shape[0]
+        if not (out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()):
+            raise AssertionError("out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()")
+        if not (out.numel() == K_shard.shape[0]):
+            raise AssertionError("out.numel() == K_shard.shape[0]")
         st = stream if stream is not None else torch.cuda.current_stream(K_shard.device)
         with torch.cuda.device(K_shard.device):
             rc = self._lib.ilre_recall_shard_scores(self._h, K_shard.data_ptr(), K_shard.shape[0],
@@ -279,8 +297,10 @@ class IlreRecall:
                  out_idx: Optional[torch.Tensor] = None,
                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Algorithm 1 on given scores (fp32 [L], finite, >= 0): ascending int32 indices."""
-        assert scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()
-        assert scores.dim() == 1
+        if not (scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()):
+            raise AssertionError("scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous()")
+        if not (scores.dim() == 1):
+            raise AssertionError("scores.dim() == 1")
         if out_idx is None:
             out_idx = torch.empty(n_sink + budget, dtype=torch.int32, device=scores.device)
         spec, _keep = _spec(max_sizes, win_sizes, win_op, n_sink)
@@ -298,9 +318,12 @@ class IlreRecall:
                  out_idx: Optional[torch.Tensor] = None, out_scores: Optional[torch.Tensor] = None,
                  stream: Optional[torch.cuda.Stream] = None):
         """Recall from HOST tensors (pinned for speed); synchronises before returning."""
-        assert not K.is_cuda and not Q.is_cuda
-        assert K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16
-        assert K.is_contiguous() and Q.is_contiguous()
+        if not (not K.is_cuda and not Q.is_cuda):
+            raise AssertionError("not K.is_cuda and not Q.is_cuda")
+        if not (K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16):
+            raise AssertionError("K.dtype == torch.bfloat16 and Q.dtype == torch.bfloat16")
+        if not (K.is_contiguous() and Q.is_contiguous()):
+            raise AssertionError("K.is_contiguous() and Q.is_contiguous()")
         L, q_len = K.shape[0], Q.shape[0]
         if out_idx is None:
             out_idx = torch.empty(n_sink + budget, dtype=torch.int32)
@@ -320,13 +343,17 @@ class IlreRecall:
         """Attention of one prefill chunk over n_prefix cached rows plus, causally, its own.
         Writes into ``out`` (bf16, Q's shape) when given."""
         for t in (Q, K, V):
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 3
+            if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 3):
+                raise AssertionError("t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 3")
         c = Q.shape[0]
-        assert Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)
-        assert K.shape == (n_prefix + c, self.cfg.n_kv_heads, self.cfg.head_dim) and V.shape == K.shape
+        if not (Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)):
+            raise AssertionError("Q.shape[1:] == (self.cfg.n_q_heads, self.cfg.head_dim)")
+        if not (K.shape == (n_prefix + c, self.cfg.n_kv_heads, self.cfg.head_dim) and V.shape == K.shape):
+            raise AssertionError("K.shape == (n_prefix + c, self.cfg.n_kv_heads, self.cfg.head_dim) and V.shape == K.shape")
         if out is None:
             out = torch.empty_like(Q)
-        assert out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == Q.shape
+        if not (out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == Q.shape):
+            raise AssertionError("out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == Q.shape")
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         rc = self._lib.ilre_recall_chunk_attention(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(),
                                                    c, n_prefix, out.data_ptr(), st.cuda_stream)
@@ -339,10 +366,14 @@ class IlreRecall:
                   stream: Optional[torch.cuda.Stream] = None) -> None:
         """Key projection + RoPE of the tokens X (positions pos0 ..) written into K_cache."""
         for t in (X, W_k, K_cache) + ((bias,) if bias is not None else ()):
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()
-        assert X.dim() == 2 and W_k.shape == (self.cfg.n_kv_heads * self.cfg.head_dim, X.shape[1])
-        assert K_cache.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert bias is None or bias.shape == (W_k.shape[0],)
+            if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()):
+                raise AssertionError("t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()")
+        if not (X.dim() == 2 and W_k.shape == (self.cfg.n_kv_heads * self.cfg.head_dim, X.shape[1])):
+            raise AssertionError("X.dim() == 2 and W_k.shape == (self.cfg.n_kv_heads * self.cfg.head_dim, X.shape[1])")
+        if not (K_cache.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)):
+            raise AssertionError("K_cache.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)")
+        if not (bias is None or bias.shape == (W_k.shape[0],)):
+            raise AssertionError("bias is None or bias.shape == (W_k.shape[0],)")
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         rc = self._lib.ilre_recall_fill_keys(
             self._h, X.data_ptr(), X.shape[0], X.shape[1], W_k.data_ptr(),
@@ -358,9 +389,12 @@ class IlreRecall:
         unless ``out`` is given.  Returns the tensor that holds the result."""
         dst = K if out is None else out
         for t in (K, dst):
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()
-            assert t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert dst.shape == K.shape
+            if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()):
+                raise AssertionError("t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()")
+            if not (t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)):
+                raise AssertionError("t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)")
+        if not (dst.shape == K.shape):
+            raise AssertionError("dst.shape == K.shape")
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         rc = self._lib.ilre_recall_rerope_keys(self._h, K.data_ptr(), dst.data_ptr(), K.shape[0],
                                                chunk_size, n_sink, float(rope_theta),
@@ -377,9 +411,12 @@ class IlreRecall:
         result.  Returns a new tensor unless ``out`` is given (``out`` may be ``K_sink``)."""
         dst = torch.empty_like(K_sink) if out is None else out
         for t in (K_sink, dst):
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()
-            assert t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert dst.shape == K_sink.shape
+            if not (t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()):
+                raise AssertionError("t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous()")
+            if not (t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)):
+                raise AssertionError("t.shape[1:] == (self.cfg.n_kv_heads, self.cfg.head_dim)")
+        if not (dst.shape == K_sink.shape):
+            raise AssertionError("dst.shape == K_sink.shape")
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         rc = self._lib.ilre_recall_rerope_sinks(self._h, K_sink.data_ptr(), dst.data_ptr(),
                                                 K_sink.shape[0], chunk_size, chunk_index,

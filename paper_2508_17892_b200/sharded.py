@@ -19,7 +19,8 @@ def shard_bounds(L: int, world: int, rank: int, align: int = 128) -> Tuple[int, 
     """[begin, end) of rank's key range: ranges are contiguous, in rank order, cover [0, L),
     and every boundary except L itself is a multiple of ``align`` (one key tile), so that no
     rank gets a ragged first tile.  Late ranks may be empty when L is small."""
-    assert L >= 0 and world >= 1 and 0 <= rank < world and align >= 1
+    if not (L >= 0 and world >= 1 and 0 <= rank < world and align >= 1):
+        raise AssertionError("L >= 0 and world >= 1 and 0 <= rank < world and align >= 1")
     tiles = (L + align - 1) // align
     lo = (tiles * rank // world) * align
     hi = (tiles * (rank + 1) // world) * align
@@ -40,7 +41,8 @@ def sharded_recall(engine, K_shard: torch.Tensor, Q: torch.Tensor, L: int, budge
     world = dist.get_world_size(group)
     rank = dist.get_rank(group)
     lo, hi = shard_bounds(L, world, rank)
-    assert K_shard.shape[0] == hi - lo, "K_shard does not match this rank's key range"
+    if not (K_shard.shape[0] == hi - lo):
+        raise AssertionError("K_shard does not match this rank's key range")
     bounds = [shard_bounds(L, world, r) for r in range(world)]
     n_rows = Q.shape[0] * Q.shape[1]
     dev = Q.device
