@@ -130,15 +130,37 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
     (lambda index: torch.cuda.current_stream(index).cuda_stream)     # (a Stream object takes microseconds)
 
 
+class _Rope(torch.autograd.Function):
+    """``rope`` where a gradient is asked for: linear, so its gradient is the transposed map of what comes back."""
+
+    @staticmethod
+    def forward(ctx, x, positions, spec, transposed):
+        ctx.save_for_backward(positions)
+        ctx.spec, ctx.transposed = spec, transposed
+        return rope(x, positions, spec, transposed)
+
+    @staticmethod
+    def backward(ctx, grad):
+        grad = grad.contiguous()
+        if grad.data_ptr() % 16:                           # a slice of a wider buffer
+            grad = grad.clone()
+        return rope(grad, ctx.saved_tensors[0], ctx.spec, not ctx.transposed), None, None, None
+
+
 def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: bool = False,
          out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """x [n_tokens, n_heads, head_dim] (bf16 or fp16; tokens may be strided) turned by int32 ``positions``.
 
     ``out`` may be ``x``.  ``transposed`` applies the transposed map: the gradient of ``rope`` with
-    respect to x is ``rope(grad, positions, spec, transposed=True)``."""
+    respect to x is ``rope(grad, positions, spec, transposed=True)``.  Differentiable with respect to x
+    where no ``out`` is given; with it a tensor that requires its gradient is refused."""
     if stream is not None:
         with _on_stream(stream, (x, positions, out)):
             return rope(x, positions, spec, transposed, out)
+    if (x.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        if out is not None:
+            raise AssertionError("out has no gradient: without it, or under torch.no_grad()")
+        return _Rope.apply(x, positions, spec, transposed)
     dtype, index = x.dtype, x.get_device()
     if index < 0 or dtype not in _DTYPES:
         raise AssertionError("x is not a bf16 or fp16 tensor of a CUDA device")

@@ -153,3 +153,81 @@ def test_append_refuses_rows_that_are_read_and_written():
             assert torch.equal(pools[0][pg, row], t["k_pool"][pg, row]) and torch.equal(pools[1][pg, row], t["v_pool"][pg, row])
     eng.check_status()
     eng.close()
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_rope_is_differentiable(transposed):
+    """A tensor that requires its gradient gets it: the transposed map of what comes back, also where that is one number
+    for all, strided or off its alignment, a second time, on a side stream and inside a captured graph."""
+    from paper_2508_17892_b200 import RopeSpec, rope
+    g = torch.Generator().manual_seed(5)
+    spec = RopeSpec(rotary_dim=64, interleaved=True, scaling="yarn", factor=8.0, orig_len=4096, low=1.0, high=32.0)
+    x, y = (torch.randn(9, 3, 128, generator=g).to(BF).cuda() for _ in range(2))
+    pos = torch.randint(0, 100000, (9,), generator=g, dtype=torch.int32).cuda()
+    turned = rope(x, pos, spec, transposed)
+    assert not turned.requires_grad
+    leaf = x.clone().requires_grad_()
+    out = rope(leaf, pos, spec, transposed)
+    assert torch.equal(out, turned) and out.requires_grad
+    back = lambda v: rope(v.clone(memory_format=torch.contiguous_format), pos, spec, not transposed)  # noqa: E731
+    want, slack = ref.rope(y.cpu(), pos.cpu(), spec, not transposed)
+    for v in (y, torch.ones((), dtype=BF, device="cuda").expand(9, 3, 128), y.flip(0).transpose(1, 2).contiguous().transpose(1, 2),
+              torch.cat([y.flatten()[:1], y.flatten()])[1:].view(9, 3, 128)):
+        grad, = torch.autograd.grad(out, leaf, v, retain_graph=True)
+        assert torch.equal(grad, back(v))
+    ref.assert_rounded(torch.autograd.grad(out, leaf, y, retain_graph=True)[0].cpu(), want, slack)
+    v = y.clone().requires_grad_()
+    grad, = torch.autograd.grad(out, leaf, v, create_graph=True)
+    assert torch.equal(torch.autograd.grad(grad, v, x)[0], turned)                      # linear: its gradient's gradient
+    (out.float() * y.float()).sum().backward()
+    assert torch.equal(leaf.grad, back(y))
+    with torch.no_grad():
+        assert not rope(leaf, pos, spec, transposed).requires_grad
+        assert rope(leaf, pos, spec, transposed, out=torch.empty_like(x)).equal(turned)
+    for into in (torch.empty_like(x), leaf):
+        with pytest.raises(AssertionError):
+            rope(leaf, pos, spec, transposed, out=into)
+    with pytest.raises(AssertionError):
+        rope(x, pos, spec, transposed, out=torch.empty_like(x).requires_grad_())
+    side = torch.cuda.Stream()
+    other = x.clone().requires_grad_()
+    side.wait_stream(torch.cuda.current_stream())
+    grad, = torch.autograd.grad(rope(other, pos, spec, transposed, stream=side), other, y)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(grad, back(y))
+    static = x.clone().requires_grad_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = rope(static, pos, spec, transposed)
+        d, = torch.autograd.grad(o, static, y)
+    with torch.no_grad():
+        static.copy_(x.flip(0))
+    y.copy_(y.flip(1))
+    graph.replay()
+    assert torch.equal(o, rope(x.flip(0), pos, spec, transposed)) and torch.equal(d, back(y))
+
+
+def test_rope_gradient_of_a_projection():
+    """Through a projection, as a model has it: the weight's gradient against 64 bits and against differences."""
+    from paper_2508_17892_b200 import RopeSpec, rope
+    g = torch.Generator().manual_seed(8)
+    spec = RopeSpec(theta=10000.0)
+    a = torch.randn(6, 32, generator=g, dtype=torch.float64)
+    w = torch.randn(32, 2 * 128, generator=g, dtype=torch.float64) / 8
+    y = torch.randn(6, 2, 128, generator=g).to(FP)
+    pos = torch.arange(6, dtype=torch.int32) * 77
+    leaf = w.float().cuda().requires_grad_()
+    rows = (a.float().cuda() @ leaf).to(FP).view(6, 2, 128)
+    (rope(rows, pos.cuda(), spec).float() * y.cuda().float()).sum().backward()
+    back, slack = ref.rope(y, pos, spec, True)               # of the rows; linear, so it does not hang on them
+    want = a.T @ back.reshape(6, 256)
+    # each of the rows' gradients is rounded once to fp16, the product of 6 terms in 32 bits
+    u = ref.half_step(FP)
+    tol = a.abs().T @ (back.abs() * u + slack * (1 + u) + 2.0 ** -25).reshape(6, 256) + 2.0 ** -20 * (a.abs().T @ back.abs().reshape(6, 256))
+    assert bool(((leaf.grad.double().cpu() - want).abs() <= tol).all())
+    f = lambda v: float((ref.rope((a @ v).view(6, 2, 128), pos, spec)[0] * y.double()).sum())  # noqa: E731
+    for i, j in ((0, 0), (17, 64), (31, 255)):
+        d = torch.zeros_like(w)
+        d[i, j] = 1e-3
+        # linear: the difference is the derivative, but for the roundings of 64 bits
+        assert abs((f(w + d) - f(w - d)) / 2e-3 - float(want[i, j])) <= 1e-8
