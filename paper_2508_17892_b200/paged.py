@@ -82,7 +82,10 @@ class RopeSpec:
 
 @dataclass(frozen=True)
 class PagedBatch:
-    """Sequences of one call (``ilre_paged_batch_t``); keeps its tensors alive."""
+    """Sequences of one call (``ilre_paged_batch_t``); keeps its tensors alive.
+
+    q_start int32 [n_seqs + 1] (None for ``evict``), kv_len int32 [n_seqs], block_table int32 [n_seqs, max_blocks],
+    contiguous and on one device."""
     q_start: Optional[torch.Tensor]
     kv_len: torch.Tensor
     block_table: torch.Tensor
@@ -90,6 +93,14 @@ class PagedBatch:
     max_q_len: int
 
     def __post_init__(self):
+        for t in (self.q_start, self.kv_len, self.block_table):
+            if t is not None and not (t.dtype == torch.int32 and t.is_contiguous() and t.device == self.kv_len.device):
+                raise AssertionError("the batch's arrays are contiguous int32 tensors of one device")
+        n = self.kv_len.numel()
+        if self.kv_len.dim() != 1 or self.block_table.dim() != 2 or self.block_table.shape[0] != n:
+            raise AssertionError("kv_len [n_seqs] and block_table [n_seqs, max_blocks]")
+        if self.q_start is not None and self.q_start.shape != (n + 1,):
+            raise AssertionError("q_start [n_seqs + 1]")
         object.__setattr__(self, "_c", IlrePagedBatch(
             self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1], _ptr(self.q_start),
             self.kv_len.data_ptr(), self.block_table.data_ptr()))
@@ -211,13 +222,8 @@ class PagedCache:
               max_q_len: int) -> PagedBatch:
         """q_start int32 [n_seqs + 1] (None for ``evict``), kv_len int32 [n_seqs] (the new tokens' rows among
         them), block_table int32 [n_seqs, max_blocks]; at most max_q_len new tokens per sequence."""
-        for t in (q_start, kv_len, block_table):
-            if not (t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous())):
-                raise AssertionError("the batch's arrays are contiguous int32 tensors of the cache's device")
-        if kv_len.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != kv_len.numel():
-            raise AssertionError("kv_len [n_seqs] and block_table [n_seqs, max_blocks]")
-        if q_start is not None and q_start.shape != (kv_len.numel() + 1,):
-            raise AssertionError("q_start [n_seqs + 1]")
+        if kv_len.device != self.device:
+            raise AssertionError("the batch's arrays are on another device")
         return PagedBatch(q_start, kv_len, block_table, n_tokens, max_q_len)
 
     def _page_step(self, t: Optional[torch.Tensor], shape) -> int:

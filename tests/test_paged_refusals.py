@@ -130,3 +130,19 @@ def test_the_bindings_have_no_assert_statements():
     for name in ("paged.py", "recall.py", "sharded.py"):
         tree = ast.parse(open(os.path.join(os.path.dirname(package.__file__), name)).read())
         assert not [n.lineno for n in ast.walk(tree) if isinstance(n, ast.Assert)], name
+
+
+def test_batches_made_by_hand_are_checked():
+    """``PagedBatch`` is public: what it is given decides how much the kernels read of it."""
+    from paper_2508_17892_b200 import PagedBatch
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)  # noqa: E731
+    wide = i32(2, 8)
+    b = PagedBatch(i32(3), i32(2), i32(2, 4), 4, 2)
+    assert (b._c.n_seqs, b._c.n_tokens, b._c.max_q_len, b._c.max_blocks) == (2, 4, 2, 4)
+    PagedBatch(None, i32(0), i32(0, 4), 0, 0)
+    for bad in ((i32(2), i32(2), i32(2, 4)), (i32(4), i32(2), i32(2, 4)), (i32(3).long(), i32(2), i32(2, 4)),
+                (i32(3), i32(2).long(), i32(2, 4)), (i32(3), i32(2), i32(2, 4).float()), (i32(3), i32(2), i32(1, 4)),
+                (i32(3), i32(2), i32(8)), (i32(3), i32(2), wide[:, :4]), (i32(3), i32(4)[::2], i32(2, 4)),
+                (i32(3), i32(1, 2), i32(2, 4)), (i32(3).to("meta"), i32(2), i32(2, 4)), (i32(3), i32(2), i32(2, 4).to("meta"))):
+        with pytest.raises(AssertionError):
+            PagedBatch(*bad, 4, 2)
