@@ -128,9 +128,11 @@ def _ints(t: torch.Tensor, index: int, n: int) -> None:
         raise AssertionError("not a contiguous int32 array of this device and length")
 
 
-def _on_stream(stream: torch.cuda.Stream, tensors):
-    """The named stream of a call: current inside, so tensors made inside are its own; the caller's tensors are
-    marked as in use by it."""
+def _on_stream(stream: torch.cuda.Stream, index: int, tensors):
+    """The named stream of a call on device `index`: current inside, so tensors made inside are its own; the caller's
+    tensors are marked as in use by it."""
+    if stream.device.index != index:
+        raise AssertionError("the stream is another device's")
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -166,7 +168,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, spec: RopeSpec, transposed: b
     respect to x is ``rope(grad, positions, spec, transposed=True)``.  Differentiable with respect to x
     where no ``out`` is given; with it a tensor that requires its gradient is refused."""
     if stream is not None:
-        with _on_stream(stream, (x, positions, out)):
+        with _on_stream(stream, x.get_device(), (x, positions, out)):
             return rope(x, positions, spec, transposed, out)
     if (x.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
         if out is not None:
@@ -260,8 +262,8 @@ class PagedCache:
         """k turned and v copied to the new tokens' rows, their weights cleared; returns q turned (``q_out``, which
         may be q; made here if not given).  spec None: nothing is turned."""
         if stream is not None:
-            with _on_stream(stream, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start, batch.kv_len,
-                                     batch.block_table)):
+            with _on_stream(stream, self._index, (q, k, v, positions, k_pool, v_pool, w_pool, q_out, batch.q_start,
+                                                  batch.kv_len, batch.block_table)):
                 return self.append(batch, q, k, v, positions, spec, k_pool, v_pool, w_pool, q_out)
         n, n_kv, dim = batch.n_tokens, self._page_shape[1], self._dim
         if k.shape[0] != n or v.shape[0] != n:
@@ -295,7 +297,7 @@ class PagedCache:
         """Every new token over its sequence's cached rows up to itself: (out like q, lse fp32 [n_tokens, n_q_heads]
         or None).  Rows of tokens that belong to no sequence are left as they are."""
         if stream is not None:
-            with _on_stream(stream, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len, batch.block_table)):
+            with _on_stream(stream, self._index, (q, k_pool, v_pool, out, lse, batch.q_start, batch.kv_len, batch.block_table)):
                 return self.attention(batch, q, k_pool, v_pool, out, lse, want_lse)
         q_stride = self._q(batch, q)
         pool = self._pool(batch, k_pool, v_pool, None)
@@ -323,7 +325,7 @@ class PagedCache:
         """Adds to w_pool the attention weight that every cached row received from the batch's new tokens (q and lse
         as ``attention`` had and returned them).  Returns w_pool."""
         if stream is not None:
-            with _on_stream(stream, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len, batch.block_table)):
+            with _on_stream(stream, self._index, (q, lse, k_pool, w_pool, batch.q_start, batch.kv_len, batch.block_table)):
                 return self.accumulate(batch, q, lse, k_pool, w_pool)
         q_stride = self._q(batch, q)
         if lse is None or w_pool is None:
@@ -345,7 +347,7 @@ class PagedCache:
         int32 [n_seqs, n_kv_heads or 1, budget], ascending, -1 behind a shorter sequence; new_len int32 [n_seqs],
         0 where a sequence's length was out of range; it may be batch.kv_len, which keeps such an entry)."""
         if stream is not None:
-            with _on_stream(stream, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len, batch.block_table)):
+            with _on_stream(stream, self._index, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len, batch.block_table)):
                 return self.evict(batch, budget, n_sink, n_recent, k_pool, v_pool, w_pool, per_head, dst_table, kept, new_len)
         n, index = batch.kv_len.numel(), self._index
         shape = (n, self._page_shape[1] if per_head else 1, budget)

@@ -146,3 +146,24 @@ def test_batches_made_by_hand_are_checked():
                 (i32(3), i32(1, 2), i32(2, 4)), (i32(3).to("meta"), i32(2), i32(2, 4)), (i32(3), i32(2), i32(2, 4).to("meta"))):
         with pytest.raises(AssertionError):
             PagedBatch(*bad, 4, 2)
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    """The kernels run on the device of the tensors; another device's stream would not be the one that they run on."""
+    from types import SimpleNamespace
+    from paper_2508_17892_b200 import paged
+    x, pos = torch.zeros(2, 1, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    used = []
+    monkeypatch.setattr(paged.torch.cuda, "stream", lambda s: used.append(s) or pytest.fail("the stream was made current"))
+    other = SimpleNamespace(device=SimpleNamespace(index=1))
+    with pytest.raises(AssertionError):
+        paged.rope(x, pos, paged.RopeSpec(), stream=other)
+    cache = paged.PagedCache.__new__(paged.PagedCache)
+    cache._index = 0
+    batch = paged.PagedBatch(torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32), 2, 1)
+    for call in (lambda: cache.append(batch, x, x, x, None, None, x, x, stream=other),
+                 lambda: cache.attention(batch, x, x, x, stream=other), lambda: cache.accumulate(batch, x, x, x, x, stream=other),
+                 lambda: cache.evict(batch, 1, 0, 0, x, x, x, stream=other)):
+        with pytest.raises(AssertionError):
+            call()
+    assert not used
