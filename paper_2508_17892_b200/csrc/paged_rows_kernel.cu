@@ -1,4 +1,4 @@
-// Attention of few query rows over the paged cache (decoding: one new token of a group of heads), single pass:
+// Attention of few query rows over the paged cache (decoding: one new token of a group of up to 16 heads), single pass:
 //   o = sum_t p_t v_t / sum_t p_t,  p_t = 2^((q.k_t) log2(e)/sqrt(d) - m),  m the running maximum.
 //
 // Bound by HBM: every key and value is read once for all heads of its group, 512 bytes for 4 x group x 128 flop.
@@ -41,15 +41,10 @@ struct RowTail {
 
 __device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
-// Rows of a tile: row r is token r / hs of the tile, head r % hs of the column (hs heads).
-struct RowShape {
-  int hs, parts;                                         // heads per column, columns per kv head
-};
-
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, kRowCtasPerSm)
 paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                  const __grid_constant__ PagedAttnParams p, const TileShape ts, const RowShape rs) {
+                  const __grid_constant__ PagedAttnParams p, const TileShape ts) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t ring = smem_u32(smem);
   float* merge = reinterpret_cast<float*>(smem + kStages * kStageBytes);          // two warps' outputs
@@ -96,7 +91,6 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     auto needs = [&](int t) { return active && t < w.p.t1 && t * kRowKeys + bx * box_rows < w.p.span.kv; };
     auto entry_at = [&](int t) -> int { return needs(t) ? table_entry(b, w.p.seq, t * kRowKeys + bx * box_rows) : 0; };
     while (more && ok) {
-      const int g = w.p.head / rs.parts;
       int e0 = entry_at(w.p.t0), e1 = entry_at(w.p.t0 + 1);
       for (int t = w.p.t0; t < w.p.t1; ++t, ++it) {
         const int s = it % kStages;
@@ -111,7 +105,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         __syncwarp();
         if (active)
-          tma_load_4d(ring + s * kStageBytes + off, is_v ? &map_v : &map_k, half * 64, g, row & (ps - 1), page, bar);
+          tma_load_4d(ring + s * kStageBytes + off, is_v ? &map_v : &map_k, half * 64, w.p.head, row & (ps - 1), page, bar);
         e0 = e1;
         e1 = e2;
       }
@@ -125,28 +119,26 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     int it = 0;
     do {
       const Piece& pc = w.p;
-      const int g = pc.head / rs.parts, h_first = g * p.group + (pc.head - g * rs.parts) * rs.hs;
-      const int heads = min(rs.hs, (g + 1) * p.group - h_first);
-      const int tok0 = pc.qt * ts.tq, n_tok = min(ts.tq, pc.span.n - tok0);
+      const int h_first = pc.head * p.group;
+      const int tok0 = pc.qt * ts.tq, n_row = min(ts.tq, pc.span.n - tok0) * p.group;
       const int pre = pc.span.kv - pc.span.n + tok0;       // token i of the tile sees rows up to pre + i
-      auto row_valid = [&](int r) { return r / rs.hs < n_tok && r % rs.hs < heads; };
-      auto row_elem = [&](int r) -> long long {            // (token, head) of row r
-        return static_cast<long long>(pc.span.q0 + tok0 + r / rs.hs);
-      };
+      // row r is token r / group of the tile, head r % group of the group
+      auto row_valid = [&](int r) { return r < n_row; };
+      auto row_tok = [&](int r) -> long long { return static_cast<long long>(pc.span.q0) + tok0 + r / p.group; };
       uint32_t qa[8][4];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int r = r0 + 8 * x;
         const bool valid = row_valid(r);
         const uint32_t* src = reinterpret_cast<const uint32_t*>(
-            static_cast<const uint16_t*>(p.q) + (valid ? row_elem(r) * p.q_stride + (h_first + r % rs.hs) * 128 : 0));
+            static_cast<const uint16_t*>(p.q) + (valid ? row_tok(r) * p.q_stride + (h_first + r % p.group) * 128 : 0));
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
           qa[ks][x] = valid ? src[ks * 8 + (c0 >> 1)] : 0u;
           qa[ks][2 + x] = valid ? src[ks * 8 + 4 + (c0 >> 1)] : 0u;
         }
       }
-      const int lim0 = pre + r0 / rs.hs, lim1 = pre + (r0 + 8) / rs.hs;
+      const int lim0 = pre + r0 / p.group, lim1 = pre + (r0 + 8) / p.group;
       float o[16][4];
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -270,7 +262,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           for (int x = 0; x < 2; ++x) {
             const int r = r0 + 8 * x;
             if (!row_valid(r) || !ok) continue;
-            const long long at = row_elem(r) * p.n_q + h_first + r % rs.hs;
+            const long long at = row_tok(r) * p.n_q + h_first + r % p.group;
             uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * 128);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -283,7 +275,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           for (int j = 0; j < 16; ++j) {
             *reinterpret_cast<float2*>(po + r0 * 128 + j * 8 + c0) = make_float2(o[j][0], o[j][1]);
           }
-          if (n_tok * rs.hs > 8) {                         // rows 8 and up, if there are any (8 x 4160 rows 34.1 -> 33.6 us)
+          if (n_row > 8) {                                  // rows 8 and up, if there are any (8 x 4160 rows 34.1 -> 33.6 us)
 #pragma unroll
             for (int j = 0; j < 16; ++j)
               *reinterpret_cast<float2*>(po + (r0 + 8) * 128 + j * 8 + c0) = make_float2(o[j][2], o[j][3]);
@@ -340,7 +332,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
             __syncwarp();
             const float inv = L == 0.f ? 0.f : 1.f / L;
-            const long long at = row_elem(r) * p.n_q + h_first + r % rs.hs;
+            const long long at = row_tok(r) * p.n_q + h_first + r % p.group;
             uint2* dst = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * 128) + lane;
             *dst = make_uint2(pack2<kF16>(acc.x * inv, acc.y * inv), pack2<kF16>(acc.z * inv, acc.w * inv));
             if (p.lse && lane == 0) p.lse[at] = (M + (log2f(L) - kShift)) * 0.69314718f;
@@ -371,12 +363,8 @@ cudaError_t init_paged_rows() {
 cudaError_t launch_paged_rows(const CUtensorMap& map_k, const CUtensorMap& map_v, const PagedAttnParams& p, bool f16,
                               int n_sm, cudaStream_t st) {
   auto k = f16 ? paged_rows_kernel<true> : paged_rows_kernel<false>;
-  // a column of work: up to 16 heads of a kv head's group
-  RowShape rs;
-  rs.hs = p.group < kRowTile ? p.group : kRowTile;
-  rs.parts = (p.group + rs.hs - 1) / rs.hs;
-  const TileShape ts = {p.n_kv * rs.parts, kRowTile / rs.hs, 6, 0};
-  return launch_after_previous(k, n_sm * kRowCtasPerSm, kThreads, kSmem, st, map_k, map_v, p, ts, rs);
+  const TileShape ts = {p.n_kv, kRowTile / p.group, 6, 0};
+  return launch_after_previous(k, n_sm * kRowCtasPerSm, kThreads, kSmem, st, map_k, map_v, p, ts);
 }
 
 }  // namespace ilre
