@@ -32,6 +32,12 @@ constexpr int kEarly = 2;                                // of a tile's four gro
 // What an item costs beside its tiles, in tiles.  Ragged batch of 12 sequences, 4096 tokens alone: 0 136 / 180 us, 2
 // 108 / 135, 3 107 / 135, 4 110 / 138.
 constexpr int kItemUnits = 3;
+// Logits against the reference take one multiply-add, whose constant is the reference in powers of two, rounded: off by up to
+// 2^-24 of it.  Every probability of the row is off by the same power then, which cancels, until it is too large for
+// its type (a logit of 10^9: 2^32 times).  So from here on (2^-5 powers) the reference is taken off first.  The test costs
+// a 128-key tile 1 % (4096 tokens alone 134.4 -> 136.8 us, 1024 behind 31744 rows 420.6 -> 425.6); two adds a logit always
+// would cost 2 to 3 %.
+constexpr float kFarLogit = 524288.f;
 constexpr int kMinUnits = 4;                             // that a CTA gets at least (64 tokens behind 4096 rows: 2 25.8 us, 4 24.9)
 
 struct ChunkTail {
@@ -343,7 +349,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             scale = (ref == -INFINITY) ? 0.f : ex2_approx((ref - cm) * c2);
             ref = (cm == -INFINITY) ? ref : cm;
           }
-          const float nr = (ref == -INFINITY) ? 0.f : fmaf(-ref, c2, kShift);
+          float nr = (ref == -INFINITY) ? 0.f : fmaf(-ref, c2, kShift);
+          if (__builtin_expect(__any_sync(0xFFFFFFFFu, fabsf(nr) > kFarLogit), 0)) {
+            const float r = (ref == -INFINITY) ? 0.f : ref;
+#pragma unroll
+            for (int j = 0; j < 128; j += 2) {
+              const float2 v = fadd2(make_float2(V(j), V(j + 1)), make_float2(-r, -r));
+              V(j) = v.x;
+              V(j + 1) = v.y;
+            }
+            nr = kShift;
+          }
           float2 sum2 = make_float2(0.f, 0.f);
           auto exponentials = [&](int g32, uint32_t (&wd)[16]) {
 #pragma unroll

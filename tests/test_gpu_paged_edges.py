@@ -231,3 +231,30 @@ def test_rope_gradient_of_a_projection():
         d[i, j] = 1e-3
         # linear: the difference is the derivative, but for the roundings of 64 bits
         assert abs((f(w + d) - f(w - d)) / 2e-3 - float(want[i, j])) <= 1e-8
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n_new", [1, 2, 40, 300])
+def test_logits_of_many_millions(n_new, dtype):
+    """Keys of 128 channels of +-30000: a query that is one of them has a logit of 10^10 there, and on every other key one
+    that is smaller by 10^8 at least.  Its probability is exactly 1 and the output that key's value, bit for bit."""
+    n_kv, n_q, kv, page = 2, 6, 900, 64
+    g = torch.Generator().manual_seed(n_new)
+    b = ref.Batch([n_new, 1], [kv, 70], page, n_kv, n_q, dtype, seed=n_new)
+    b.k_pool = ((torch.randint(0, 2, b.k_pool.shape, generator=g) * 2 - 1) * 30000.0).to(dtype)
+    want = torch.zeros_like(b.q)
+    for i, (m, rows) in enumerate(((n_new, kv), (1, 70))):
+        pg, row = b.slots(i)
+        for j in range(m):
+            for h in range(n_q):
+                t = int(torch.randint(0, rows - m + j + 1, (), generator=g))
+                b.q[b.starts[i] + j, h] = b.k_pool[pg[t], row[t], h * n_kv // n_q]
+                want[b.starts[i] + j, h] = b.v_pool[pg[t], row[t], h * n_kv // n_q]
+    eng = _engine(b)
+    t = b.gpu(eng)
+    out, lse = eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], want_lse=True)
+    eng.check_status()
+    assert torch.equal(out.cpu(), want)
+    top = 128 ** 0.5 * float(b.k_pool.flatten()[0].abs()) ** 2
+    assert float((lse.double().cpu() / top - 1).abs().max()) <= 2.0 ** -20
+    eng.close()
