@@ -496,8 +496,8 @@ int ilre_paged_append(ilre_paged_t* h, const ilre_paged_batch_t* batch, const il
  * from q_dev.  A token that sees nothing (kv_len[i] < n_i) gets zeros and lse -infinity.  Rows at kv_len[i]
  * and beyond may hold anything, NaN included; keys and values of rows below it must be finite.  Pages may be
  * shared.  Products on the tensor cores, fp32 sums; the probabilities are rounded to the cache's type before
- * they multiply the values, as the output is (fp16: those below 2^-32 of the row's largest are rounded to a multiple of
- * 2^-31 of it).  Logits may be as large as fp32 holds.
+ * they multiply the values, as the output is (fp16: those below 2^-21 of the row's largest to a multiple of 2^-31
+ * of it).  Logits may be as large as fp32 holds.
  */
 int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev,
                          int64_t q_stride, const ilre_paged_pool_t* pool, void* out_dev,
@@ -508,8 +508,8 @@ int ilre_paged_attention(ilre_paged_t* h, const ilre_paged_batch_t* batch, const
  *   w[t, g] += sum over the heads h of kv head g and the new tokens j that see t of
  *              exp(q[j, h, :] . k[t, g, :] / sqrt(128) - lse[j, h])
  * with q and lse as in ilre_paged_attention.  Sums in fp32, and so is the exponent: a weight is off by up to
- * 2^-22 (|logit| + |lse|) of itself (3e-5 at logits of 100), which logits beyond 10^5 leave little of; a page that several sequences of the batch
- * share receives all of theirs (in an order that may vary; without sharing results repeat bit by bit).
+ * 2^-22 (|logit| + |lse|) of itself (3e-5 at logits of 100).  A page that several sequences of the batch share receives
+ * all of theirs (in an order that may vary; without sharing results repeat bit by bit).
  */
 int ilre_paged_accumulate(ilre_paged_t* h, const ilre_paged_batch_t* batch, const void* q_dev,
                           int64_t q_stride, const float* lse_dev, const ilre_paged_pool_t* pool,

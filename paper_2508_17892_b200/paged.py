@@ -202,6 +202,7 @@ class PagedCache:
 
     k_pool, v_pool: [n_pages, page_size, n_kv_heads, 128], pages contiguous (the stride from page to page is
     free, so the two may be halves of one tensor); w_pool: fp32 [n_pages, n_kv_heads, page_size].
+    For serving: results carry no graph, whatever the tensors require (``rope`` alone is differentiable).
     One stream at a time; graphs that hold calls of one handle must not run at the same time."""
 
     def __init__(self, n_kv_heads: int = 8, n_q_heads: int = 32, page_size: int = 64,
