@@ -238,7 +238,11 @@ class PagedCache:
         step = t.stride()
         if not (step[1:] == self._page_stride or shape[0] == 0 or t[0].is_contiguous()):
             raise AssertionError("a page is not contiguous")
-        return step[0] if shape[0] > 1 else 0
+        if shape[0] <= 1:
+            return 0
+        if step[0] == 0:                                   # to the library that would say back to back
+            raise AssertionError("the pool is one page shown many times")
+        return step[0]
 
     def _pool(self, batch: PagedBatch, k: torch.Tensor, v: Optional[torch.Tensor], w: Optional[torch.Tensor]) -> IlrePagedPool:
         if batch.index != self._index:

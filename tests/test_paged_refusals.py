@@ -167,3 +167,45 @@ def test_streams_of_another_device_are_refused(monkeypatch):
         with pytest.raises(AssertionError):
             call()
     assert not used
+
+
+def _host_cache(monkeypatch=None):
+    """A cache without a handle, as if the host's tensors were its device's, and the calls that reached its library."""
+    from paper_2508_17892_b200 import paged
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append((name, a)) or 0
+
+    c = paged.PagedCache.__new__(paged.PagedCache)
+    c._lib, c._h, c.dtype, c._n_q, c._dim, c._index, c.device = Library(), None, torch.bfloat16, 8, 128, -1, torch.device("cpu")
+    c._page_shape, c._weight_shape, c._page_stride = (16, 2, 128), (2, 16), (256, 128, 1)
+    if monkeypatch is not None:
+        monkeypatch.setattr(paged, "_raw_stream", lambda index: 0)
+    return c, calls
+
+
+def test_pools_of_one_page_shown_many_times_are_refused(monkeypatch):
+    """A pool that is one page expanded has a stride of 0 from page to page, which the C call reads as back to back: pages
+    that are not there.  Pages that overlap are left to the C call, which refuses their stride."""
+    from paper_2508_17892_b200 import PagedBatch
+    c, calls = _host_cache(monkeypatch)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)  # noqa: E731
+    b = PagedBatch(i32(3), i32(2), i32(2, 4), 4, 2)
+    q, k = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(4, 2, 128, dtype=torch.bfloat16)
+    page, pool, w = torch.zeros(1, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 16)
+    shown = page.expand(3, 16, 2, 128)
+    for kp, vp in ((shown, pool), (pool, shown), (shown, shown)):
+        for call in (lambda: c.attention(b, q, kp, vp), lambda: c.append(b, q, k, k, None, None, kp, vp),
+                     lambda: c.evict(b, 8, 0, 0, kp, vp, w)):
+            with pytest.raises(AssertionError):
+                call()
+    with pytest.raises(AssertionError):
+        c.accumulate(b, q, torch.zeros(4, 8), shown, w)
+    assert not calls
+    c.attention(b, q, page, page)                            # one page, shown once
+    c.attention(b, q, page.expand(1, 16, 2, 128), page)
+    c.attention(b, q, pool, torch.zeros(3, 2, 16, 2, 128, dtype=torch.bfloat16)[:, 0])
+    strides = [a[4]._obj.v_page_stride for _, a in calls]
+    assert strides == [0, 0, 2 * 16 * 2 * 128]
