@@ -54,6 +54,13 @@ def declare(lib: ctypes.CDLL) -> None:
         getattr(lib, "ilre_paged_" + name).argtypes = [vp]
 
 
+def _int32(*values: int) -> None:
+    """What goes into 32 bits of a C structure; ctypes would cut off the rest."""
+    for v in values:
+        if not -(1 << 31) <= v < 1 << 31:
+            raise AssertionError("a number of more than 32 bits")
+
+
 @dataclass(frozen=True)
 class RopeSpec:
     """Rotary positions: layout, rotated part of the head and scaling (see ``ilre_rope_spec_t``).
@@ -71,6 +78,7 @@ class RopeSpec:
     attn_factor: float = 0.0
 
     def __post_init__(self):
+        _int32(self.rotary_dim)
         object.__setattr__(self, "_c", IlreRopeSpec(
             self.theta, self.rotary_dim, int(self.interleaved), _SCALINGS[self.scaling], self.factor, self.orig_len,
             self.low, self.high, self.attn_factor))
@@ -101,6 +109,7 @@ class PagedBatch:
             raise AssertionError("kv_len [n_seqs] and block_table [n_seqs, max_blocks]")
         if self.q_start is not None and self.q_start.shape != (n + 1,):
             raise AssertionError("q_start [n_seqs + 1]")
+        _int32(self.n_tokens, self.max_q_len)
         object.__setattr__(self, "_c", IlrePagedBatch(
             self.kv_len.numel(), self.n_tokens, self.max_q_len, self.block_table.shape[1], _ptr(self.q_start),
             self.kv_len.data_ptr(), self.block_table.data_ptr()))
@@ -207,6 +216,7 @@ class PagedCache:
 
     def __init__(self, n_kv_heads: int = 8, n_q_heads: int = 32, page_size: int = 64,
                  dtype: torch.dtype = torch.bfloat16, max_seqs: int = 256, head_dim: int = 128, device: int = 0):
+        _int32(n_kv_heads, n_q_heads, page_size, max_seqs, head_dim, device)
         self._lib = load_library()
         self._h = ctypes.c_void_p()
         self.cfg = IlrePagedConfig(n_kv_heads, n_q_heads, head_dim, page_size, _DTYPES[dtype], max_seqs, device)
@@ -354,6 +364,7 @@ class PagedCache:
         if stream is not None:
             with _on_stream(stream, self._index, (k_pool, v_pool, w_pool, dst_table, kept, new_len, batch.kv_len, batch.block_table)):
                 return self.evict(batch, budget, n_sink, n_recent, k_pool, v_pool, w_pool, per_head, dst_table, kept, new_len)
+        _int32(budget, n_sink, n_recent)
         n, index = batch.kv_len.numel(), self._index
         shape = (n, self._page_shape[1] if per_head else 1, budget)
         if budget < 1 or w_pool is None:

@@ -209,3 +209,27 @@ def test_pools_of_one_page_shown_many_times_are_refused(monkeypatch):
     c.attention(b, q, pool, torch.zeros(3, 2, 16, 2, 128, dtype=torch.bfloat16)[:, 0])
     strides = [a[4]._obj.v_page_stride for _, a in calls]
     assert strides == [0, 0, 2 * 16 * 2 * 128]
+
+
+def test_numbers_of_more_than_32_bits_are_refused(monkeypatch):
+    """The C structures hold 32 bits; ctypes would cut a larger number down to its low ones."""
+    from paper_2508_17892_b200 import PagedBatch, PagedCache, RopeSpec
+    c, calls = _host_cache(monkeypatch)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)  # noqa: E731
+    big = 1 << 32
+    for kw in (dict(n_tokens=big + 4), dict(max_q_len=big + 1), dict(n_tokens=1 << 31), dict(max_q_len=-big)):
+        with pytest.raises(AssertionError):
+            PagedBatch(i32(3), i32(2), i32(2, 4), **{**dict(n_tokens=4, max_q_len=2), **kw})
+    with pytest.raises(AssertionError):
+        RopeSpec(rotary_dim=big + 64)
+    for name in ("n_kv_heads", "n_q_heads", "page_size", "max_seqs", "head_dim", "device"):
+        with pytest.raises(AssertionError):
+            PagedCache(**{name: big + 64})
+    b = PagedBatch(None, i32(0), i32(0, 4), 0, 0)
+    pool, w = torch.zeros(3, 16, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 16)
+    for budget, sink, recent in ((big + 8, 0, 0), (8, big, 0), (8, 0, big), (8, 1 - big, 0), (8, 0, 1 - big)):
+        with pytest.raises(AssertionError):
+            c.evict(b, budget, sink, recent, pool, pool, w)
+    assert not calls
+    c.evict(b, (1 << 31) - 1, 0, 0, pool, pool, w)           # the C call's to refuse
+    assert len(calls) == 1
