@@ -98,7 +98,12 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
   const bool ok = kv >= 0 && kv <= (static_cast<long long>(p.batch.max_blocks) << p.batch.page_shift);
   if (!ok && threadIdx.x == 0) report(p.batch.status, kDevBadLengths);
   const int n_keep = ok ? min(kv, p.budget) : 0;
-  if (threadIdx.x == 0 && rank == 0 && list == 0) p.n_keep[seq] = ok ? n_keep : -1;
+  if (threadIdx.x == 0 && rank == 0 && list == 0) {
+    p.n_keep[seq] = ok ? n_keep : -1;
+    // A sequence left out has no rows; the batch's own array keeps what it says, so that the next call reports it too.
+    // (The kernels that move rows write the other lengths.)
+    if (!ok && p.new_len != p.batch.kv_len) p.new_len[seq] = 0;
+  }
   if (!ok || kv <= p.budget) {                           // the whole cluster
     for (int i = rank * kSelThreads + threadIdx.x; i < p.budget; i += n_cta * kSelThreads) kept[i] = i < n_keep ? i : -1;
     return;
@@ -190,12 +195,6 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
   }
 }
 
-// n: rows that the sequence keeps, -1 where its length is out of range: no rows then, but the batch's own array keeps what
-// it says, so that the next call reports it too.
-__device__ __forceinline__ void write_length(const EvictParams& p, int seq, int n) {
-  if (n >= 0) p.new_len[seq] = n;
-  else if (p.new_len != p.batch.kv_len) p.new_len[seq] = 0;
-}
 __device__ __forceinline__ int dst_page(const EvictParams& p, int seq, int i) {
   return checked_page(p.batch, p.dst_table[static_cast<long long>(seq) * p.dst_blocks + (i >> p.batch.page_shift)]);
 }
@@ -212,7 +211,7 @@ evict_copy_kernel(const __grid_constant__ EvictParams p) {
   grid_dep_launch();
   const PagedBatch& b = p.batch;
   const int n = p.n_keep[seq], mask = (1 << b.page_shift) - 1;
-  if (g == 0 && i0 == 0 && threadIdx.x == 0) write_length(p, seq, n);
+  if (g == 0 && i0 == 0 && threadIdx.x == 0 && n >= 0) p.new_len[seq] = n;
   if (i0 >= n) return;
   if (threadIdx.x < kMoveRows) {
     const int i = i0 + threadIdx.x;
@@ -265,9 +264,9 @@ evict_move_kernel(const __grid_constant__ EvictParams p) {
   grid_dep_wait();
   grid_dep_launch();
   const int n = p.n_keep[seq];
-  if (col == 0 && g == 0 && threadIdx.x == 0) write_length(p, seq, n);
   if (n < 0) return;
   const PagedBatch& b = p.batch;
+  if (col == 0 && g == 0 && threadIdx.x == 0) p.new_len[seq] = n;
   const int32_t* kept = kept_rows(p, seq, g);
   int first = 0;                                         // kept[i] - i never falls: the first row that moves
   for (int hi = n; first < hi;) {
