@@ -98,14 +98,12 @@ evict_select_kernel(const __grid_constant__ EvictParams p, int keep, int n_cta) 
   const bool ok = kv >= 0 && kv <= (static_cast<long long>(p.batch.max_blocks) << p.batch.page_shift);
   if (!ok && threadIdx.x == 0) report(p.batch.status, kDevBadLengths);
   const int n_keep = ok ? min(kv, p.budget) : 0;
-  if (threadIdx.x == 0 && rank == 0 && list == 0) {
-    p.n_keep[seq] = ok ? n_keep : -1;
-    // A sequence left out has no rows; the batch's own array keeps what it says, so that the next call reports it too.
-    // (The kernels that move rows write the other lengths.)
-    if (!ok && p.new_len != p.batch.kv_len) p.new_len[seq] = 0;
-  }
+  if (threadIdx.x == 0 && rank == 0 && list == 0) p.n_keep[seq] = ok ? n_keep : -1;
   if (!ok || kv <= p.budget) {                           // the whole cluster
     for (int i = rank * kSelThreads + threadIdx.x; i < p.budget; i += n_cta * kSelThreads) kept[i] = i < n_keep ? i : -1;
+    // A sequence left out has no rows; the batch's own array keeps what it says, so that the next call reports it too.
+    // (The kernels that move rows write the other lengths.)
+    if (!ok && p.new_len != p.batch.kv_len && threadIdx.x == 0 && rank == 0 && list == 0) p.new_len[seq] = 0;
     return;
   }
   for (int i = rank * kSelThreads + threadIdx.x; i < p.n_sink; i += n_cta * kSelThreads) kept[i] = i;
