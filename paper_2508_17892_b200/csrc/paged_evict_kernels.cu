@@ -253,8 +253,8 @@ evict_copy_kernel(const __grid_constant__ EvictParams p) {
 
 // In place: CTA x of a head has column x of its keys or values, the last one its weights.  Rows that stay lead the list
 // (kept[i] = i) and are passed over.  kMoveFlight: rows of a thread in flight, 8 where the launch leaves SMs
-// to spare and a CTA's own rate counts, 2 where many CTAs share them (one request of 4608 rows 38 us with 8, 42 with 2; 16
-// prompts of 6000 to 14000 rows 209 with 8, 138 with 2).
+// to spare and a CTA's own rate counts, 2 where many CTAs share them (one request of 4608 rows 36 us with 8, 42 with 2; 16
+// prompts of 6000 to 14000 rows 209 with 8, 137 with 2: 32 registers, so that all its CTAs run as one wave).
 template <int kMoveFlight>
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(const __grid_constant__ EvictParams p) {
@@ -350,7 +350,8 @@ cudaError_t launch_evict(const EvictParams& p, int n_sm, cudaStream_t st) {
   const long long rows = static_cast<long long>(p.batch.max_blocks) << p.batch.page_shift;
   // Few CTAs for short lists: what a CTA reads of the others' histograms grows with their number (24 KB each, the
   // longest step: one request of 4608 rows, eight lists, with all three 18.9 us with 8 CTAs, 15.0 with 2, then 13.8 with
-  // 2, 16.0 with 1; 16 lists of 6000 to 14000 rows 115 with 8, 108 with 4).
+  // 2, 16.0 with 1; 16 lists of 6000 to 14000 rows 115 with 8, 108 with 4).  The table's width is all that the host
+  // knows of the lists: 4608 rows in a table of 16384 take 13.4, in one of 32768, with 8 CTAs, 16.3.
   const int n_cta = rows <= 8192 ? 2 : rows <= 16384 ? 4 : kSelCluster;
   const long long part = (rows + n_cta - 1) / n_cta;
   const int keep = static_cast<int>(part < kSelKeep ? (part + 3) & ~3ll : kSelKeep);

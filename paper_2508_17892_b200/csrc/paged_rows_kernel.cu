@@ -26,7 +26,7 @@ constexpr int kWarps = 4;                                // consumers
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kMergeFloats = kRowTile * 128;             // output of one warp on its way to another
 constexpr int kJoinFlight = 8;                           // partial results in flight
-constexpr int kMinUnits = 3;                             // 64-key tiles that a CTA gets at least (4160 rows: 2 12.8 us, 3 12.1, 4 14.7)
+constexpr int kMinUnits = 3;                             // 64-key tiles that a CTA gets at least (4160 rows: 2 11.8 us, 3 11.2, 4 13.6; 32768 rows alike)
 
 struct RowTail {
   uint64_t full[kStages];

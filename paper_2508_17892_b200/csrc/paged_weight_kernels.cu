@@ -11,7 +11,10 @@
 // four groups of four warps (the parity of the unit by the half of the keys) have two accumulators each, so that the next
 // unit's logits are there when a group has summed up this one's.  256 x 64 logits then take 1225 cycles, 84 % of the
 // units' rate; a fourth of them as polynomials on the FMA pipe made it slower.  A 4160-token prompt (32 / 8 heads): 99 us,
-// 717 TFLOP/s.  (One unit at a time per group, 128 rows: 122 us; two groups that take 128 logits to registers: 129 us.)
+// 720 TFLOP/s.  (One unit at a time per group, 128 rows: 122 us; two groups that take 128 logits to registers: 129 us.)
+//
+// Nothing is rounded to fewer than 32 bits: logits, exponents, the approximate exponential (2 ulp) and sums.  Against 64 bits
+// that prompt's weights are 4.4e-7 off (exp of torch in 32 bits 0.8e-7).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
