@@ -258,3 +258,90 @@ def test_logits_of_many_millions(n_new, dtype):
     top = 128 ** 0.5 * float(b.k_pool.flatten()[0].abs()) ** 2
     assert float((lse.double().cpu() / top - 1).abs().max()) <= 2.0 ** -20
     eng.close()
+
+
+def test_as_many_kv_heads_as_are_taken():
+    """1024 kv heads: appended, attended (few rows and chunks), weighed, cut in place and to other pages."""
+    b = ref.Batch([3, 20, 1], [40, 20, 17], 16, 1024, 1024, seed=12, spare=4).poison()
+    eng = _engine(b)
+    t = b.gpu(eng)
+    out, lse = eng.attention(t["batch"], t["q"], t["k_pool"], t["v_pool"], want_lse=True)
+    want, want_lse, tol, tol_lse = ref.attention(b)
+    assert bool(((out.double().cpu() - want).abs() <= tol).all())
+    assert bool(((lse.double().cpu() - want_lse).abs() <= tol_lse).all())
+    w = t["w_pool"].clone()
+    eng.accumulate(t["batch"], t["q"], lse, t["k_pool"], w)
+    want_w, tol_w = ref.accumulate(b, lse.cpu())
+    assert bool(((w.double().cpu() - want_w).abs() <= tol_w).all())
+    for per_head in (True, False):
+        kept = ref.evict_choice(b, 16, 1, 5, per_head)
+        k, v, wp = t["k_pool"].clone(), t["v_pool"].clone(), t["w_pool"].clone()
+        got, n = eng.evict(t["batch"], 16, 1, 5, k, v, wp, per_head=per_head)
+        dst = torch.tensor(b.free[:3], dtype=torch.int32)[:, None]
+        k2, v2, wp2 = t["k_pool"].clone(), t["v_pool"].clone(), t["w_pool"].clone()
+        got2, _ = eng.evict(t["batch"], 16, 1, 5, k2, v2, wp2, per_head=per_head, dst_table=dst.cuda())
+        assert n.tolist() == [16, 16, 16] and torch.equal(got, got2) and got.cpu().tolist() == kept
+        for i in range(3):
+            a, c = b.table[i, 0], dst[i, 0]
+            pg, row = b.slots(i)
+            src = got[i].long().cpu().expand(1024, 16)
+            heads = torch.arange(1024)[:, None]
+            want_k = b.k_pool[pg[src], row[src], heads].transpose(0, 1)
+            assert torch.equal(k[a].cpu(), want_k) and torch.equal(k2[c].cpu(), want_k)
+            assert torch.equal(v[a], v2[c]) and torch.equal(wp[a], wp2[c])
+            assert torch.equal(wp[a].cpu(), b.w_pool[pg[src], heads, row[src]])
+    new = eng.append(t["batch"], t["q"], t["k"], t["v"], None, None, t["k_pool"], t["v_pool"], t["w_pool"])
+    assert torch.equal(new, t["q"])
+    for i in range(3):
+        pg, row = (x[b.kv_len_list[i] - b.q_len[i]:].cuda() for x in b.slots(i))
+        assert torch.equal(t["k_pool"][pg, row], t["k"][b.starts[i]:b.starts[i + 1]])
+        assert torch.equal(t["v_pool"][pg, row], t["v"][b.starts[i]:b.starts[i + 1]]) and not bool(t["w_pool"][pg, :, row].any())
+    eng.check_status()
+    assert eng.check_guards() == 0
+    eng.close()
+
+
+def test_as_many_sequences_as_are_taken():
+    """65535 sequences of one to three rows on a page each, the newest row of this call: every operator once."""
+    from paper_2508_17892_b200 import PagedCache, RopeSpec
+    n = 65535
+    g = torch.Generator(device="cuda").manual_seed(3)
+    eng = PagedCache(n_kv_heads=1, n_q_heads=2, page_size=16, max_seqs=n)
+    k_pool, v_pool = (torch.randn(n, 16, 1, 128, generator=g, device="cuda").to(BF) for _ in range(2))
+    w_pool = torch.rand(n, 1, 16, generator=g, device="cuda")
+    table = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[:, None].contiguous()
+    kv = (torch.arange(n, device="cuda") % 3 + 1).to(torch.int32)
+    batch = eng.batch(torch.arange(n + 1, dtype=torch.int32, device="cuda"), kv, table, n, 1)
+    q, k, v = (torch.randn(n, h, 128, generator=g, device="cuda").to(BF) for h in (2, 1, 1))
+    page, last = table[:, 0].long(), kv.long() - 1
+    qr = eng.append(batch, q, k, v, last.to(torch.int32), RopeSpec(), k_pool, v_pool, w_pool)
+    assert torch.equal(v_pool[page, last], v) and not bool(w_pool[page, 0, last].any())
+    out, lse = eng.attention(batch, qr, k_pool, v_pool, want_lse=True)
+    s = torch.einsum("nhd,nkd->nhk", qr.double(), k_pool[page][:, :3, 0].double()) / 128 ** 0.5
+    s = s.masked_fill(torch.arange(3, device="cuda") > last[:, None, None], float("-inf"))
+    z = torch.logsumexp(s, dim=-1)
+    p = torch.exp(s - z[..., None])
+    vals = v_pool[page][:, :3, 0].double()
+    # logits off by 2^-17 at most (128 products of sizes below 2^5 in 32 bits, their sum below 2^9), the probabilities and
+    # the output rounded to bf16
+    u = ref.half_step(BF)
+    want = torch.einsum("nhk,nkd->nhd", p, vals)
+    tol = u * want.abs() + (u + 2.0 ** -15) * (1 + u) * torch.einsum("nhk,nkd->nhd", p, vals.abs()) + 1e-30
+    assert bool(((out.double() - want).abs() <= tol).all())
+    assert float((lse.double() - z).abs().max()) <= 2.0 ** -14
+    before = w_pool.clone()
+    eng.accumulate(batch, qr, lse, k_pool, w_pool)
+    gain = (w_pool - before)[page][:, 0, :3].double()
+    assert float((gain - p.sum(dim=1)).abs().max()) <= 2 * (2.0 ** -14 + 2.0 ** -20) + 2.0 ** -22
+    kept, new_len = eng.evict(batch, 2, 0, 1, k_pool, v_pool, w_pool)
+    assert torch.equal(new_len, kv.clamp(max=2))
+    w3 = before[page][:, 0, :3].double() + gain
+    heavier = (w3[:, 1] > w3[:, 0]).long()
+    three = kv == 3
+    assert torch.equal(kept[three, 0, 1], torch.full((int(three.sum()),), 2, dtype=torch.int32, device="cuda"))
+    clear = three & ((w3[:, 1] - w3[:, 0]).abs() > 1e-3)
+    assert int(clear.sum()) > 15000 and torch.equal(kept[clear, 0, 0].long(), heavier[clear])
+    assert bool((kept[kv == 1, 0] == torch.tensor([0, -1], dtype=torch.int32, device="cuda")).all())
+    eng.check_status()
+    assert eng.check_guards() == 0
+    eng.close()
