@@ -201,8 +201,10 @@ float softmax_scale() { return static_cast<float>(1.4426950408889634 / std::sqrt
 
 // Sequences whose rows (new tokens x heads of a group) fit one tile of 16 are bound by the reading of the cache and
 // go to the row kernels; the others' rows share a key tile in the tensor-core kernels.  The launches follow from what
-// the host knows: one sequence has one kind, and max_q_len may rule out the second.  (Eight sequences of 16000 rows,
-// 32 / 8 heads: 4 new tokens 96 us by rows; 5 tokens 146 us by rows, in two tiles, 111 us in the chunk kernel.)
+// the host knows: one sequence has one kind, and max_q_len may rule out the second.  (32 / 8 heads, us by the chunk kernel
+// / by rows in tiles of 16: 5 new tokens behind 500 rows 17.0 / 17.2, behind 4096 18.4 / 21.9, 16000 25.6 / 30.5; 16
+// sequences of them 21.5 / 22.3, 70 / 65, 194 / 210; of 16 new tokens 24 / 33, 72 / 122, 196 / 411.  Up to 4 new tokens,
+// one tile: 8 sequences of 16000 rows 95 by rows, 111 in the chunk kernel.)
 struct KernelChoice {
   int row_tokens;                                        // most new tokens of the first kind; 0: more than 16 heads
   bool rows, chunks;
