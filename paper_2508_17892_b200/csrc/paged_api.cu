@@ -149,9 +149,10 @@ int validate_rows(const void* base, int64_t stride, int64_t heads, int head_dim)
 // apart even where they alternate (slices of one tensor); with two strides the spans count.
 bool rows_overlap(const void* a, int64_t a_stride, int64_t a_row, const void* b, int64_t b_stride, int64_t b_row, int64_t n) {
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  if (a0 >= b0 + static_cast<uintptr_t>((n - 1) * b_stride + b_row) * 2 ||
-      b0 >= a0 + static_cast<uintptr_t>((n - 1) * a_stride + a_row) * 2)
-    return false;
+  const auto bytes = [n](int64_t stride, int64_t row) -> uintptr_t {       // no memory is as long as would wrap
+    return (static_cast<uintptr_t>(n - 1) * static_cast<uintptr_t>(stride) + static_cast<uintptr_t>(row)) * 2;
+  };
+  if (a0 >= b0 + bytes(b_stride, b_row) || b0 >= a0 + bytes(a_stride, a_row)) return false;
   if (n == 1 || a_stride != b_stride) return true;
   const int64_t step = a_stride * 2, apart = static_cast<int64_t>(b0 - a0) % step;
   const int64_t behind = apart < 0 ? apart + step : apart;     // from a row of a to the next one of b
